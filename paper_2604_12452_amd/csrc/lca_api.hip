@@ -6,11 +6,15 @@
 #include <cstring>
 #include <mutex>
 
-#include "lca_internal.h"
+#include "api_checks.h"
 
 namespace {
 
 thread_local char g_err[512] = "";
+
+}  // namespace
+
+namespace lca {
 
 lca_status fail(lca_status st, const char *fmt, ...)
 {
@@ -21,7 +25,14 @@ lca_status fail(lca_status st, const char *fmt, ...)
     return st;
 }
 
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+}  // namespace lca
+
+namespace {
+
+using lca::aligned16;
+using lca::check_ptr;
+using lca::fail;
+using lca::hip_status;
 
 // Validate the descriptor and derive sizes. `decode`: L counts the token being decoded.
 lca_status make_dims(const lca_desc *desc, lca::Dims &d)
@@ -68,19 +79,6 @@ size_t workspace_bytes(const lca::Dims &d)
     return need > dev ? need : dev;
 }
 
-lca_status check_ptr(const void *p, const char *name, bool required = true)
-{
-    if (p == nullptr) return required ? fail(LCA_ERR_INVALID_ARG, "%s is NULL", name) : LCA_OK;
-    if (!aligned16(p)) return fail(LCA_ERR_INVALID_ARG, "%s is not 16-byte aligned", name);
-    return LCA_OK;
-}
-
-#define LCA_TRY(expr)                      \
-    do {                                   \
-        lca_status _s = (expr);            \
-        if (_s != LCA_OK) return _s;       \
-    } while (0)
-
 lca_status check_ws(const lca::Dims &d, const void *ws, size_t ws_bytes)
 {
     const size_t need = workspace_bytes(d);
@@ -90,17 +88,6 @@ lca_status check_ws(const lca::Dims &d, const void *ws, size_t ws_bytes)
     if (ws_bytes < need) return fail(LCA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, need);
     return LCA_OK;
 }
-
-lca_status hip_status(hipError_t e, const char *what)
-{
-    if (e == hipSuccess) return LCA_OK;
-    return fail(LCA_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-}
-
-// The launch functions report hipGetLastError() after their kernels, and that call returns the calling thread's last
-// error whoever caused it: one left behind by an earlier runtime call of the caller's own would be taken for a failed
-// launch.  So the thread's error state is read, and thereby cleared, right before a launch function runs.
-#define LCA_LAUNCH(call, what) ((void)hipGetLastError(), hip_status((call), (what)))
 
 // The two layer-width kernels take their widths in a 16-bit type with a positive scale (their fixed-reference softmax
 // orders logits by the raw products); the tiled kernel takes every other descriptor, a zero or negative scale included, that it has an

@@ -1,0 +1,113 @@
+// Internal declarations of the serving operators (include/lca_serve.h): validated sizes, arguments, launchers, and the
+// few device functions that their kernels share.
+#pragma once
+#include "lanes.h"
+#include "lca_internal.h"
+#include "lca_serve.h"
+
+namespace lca {
+
+// A validated lca_serve_desc; rows resolved, hints resolved (max_kv <= max_blocks * page, max_q <= T).
+struct ServeDims {
+    int B, T, H, S, hps, d_pool, d_sel, dtype;
+    int page, n_blocks, max_blocks, max_q, max_kv, window;
+    float scale, softcap;
+    size_t q_row, sel_row, pool_row;
+};
+
+struct TablesArgs {
+    ServeDims d;
+    const int32_t *cached_len, *new_len, *free_list, *free_count;
+    int32_t *free_left, *block_table, *q_start, *seq_len, *slot, *position, *request;
+    int32_t *base;                 // workspace, [B]
+};
+hipError_t launch_page_tables(const TablesArgs &a, hipStream_t st);
+
+struct ReleaseArgs {
+    ServeDims d;
+    const int32_t *finished;
+    int32_t *cached_len, *block_table, *free_list, *free_count;
+};
+hipError_t launch_page_release(const ReleaseArgs &a, hipStream_t st);
+
+struct StoreArgs {
+    ServeDims d;
+    const void *SEL, *POOL;
+    const int32_t *slot;
+    uint8_t *sel_q8, *pool_q8;
+    float *scales;
+};
+hipError_t launch_page_store_q8(const StoreArgs &a, hipStream_t st);
+
+// Both attention calls: packed (block_table == NULL: keys and values are SEL, POOL) or over the cache.
+struct ScoredArgs {
+    ServeDims d;
+    const void *Q, *SEL, *POOL;
+    const int32_t *q_start, *seq_len, *prefix_len, *block_table;
+    const float *slopes;
+    const uint8_t *sel_q8, *pool_q8;
+    const float *scales;
+    void *O;
+    float *lse;
+    float *part;                   // workspace: split partials
+};
+hipError_t launch_scored_rows(const ScoredArgs &a, hipStream_t st);
+
+// ---- device functions ----
+
+constexpr float LOG2E = 1.4426950408889634f;
+
+// The score rule in base 2: what the kernels need per call.  With a cap, cap * tanh(x) = cap - 2 cap / (1 + e^(2x)): two
+// hardware instructions at a quarter rate, exact to a few 2^-24 of the cap, and its limits are right at infinities.
+struct ScoreRule {
+    float scale_log2;              // no cap: logit (base 2) = dot * scale_log2
+    float pre, cap_log2;           // cap: logit = cap_log2 - 2 cap_log2 / (1 + 2^(dot * pre)); cap_log2 = 0: no cap
+    int window;                    // INT_MAX: none
+};
+inline ScoreRule score_rule(const ServeDims &d)
+{
+    ScoreRule r;
+    r.scale_log2 = d.scale * LOG2E;
+    r.cap_log2 = d.softcap * LOG2E;
+    r.pre = d.softcap > 0.f ? 2.f * d.scale / d.softcap * LOG2E : 0.f;
+    r.window = d.window > 0 ? d.window : 0x7FFFFFFF;
+    return r;
+}
+template <bool CAP> __device__ __forceinline__ float capped(float dot, const ScoreRule &r)
+{
+    if constexpr (!CAP) return dot * r.scale_log2;
+    const float e = __builtin_amdgcn_exp2f(dot * r.pre);
+    return fmaf(-2.f * r.cap_log2, __builtin_amdgcn_rcpf(1.f + e), r.cap_log2);
+}
+
+// The request whose rows hold row t: the last one that starts at or in front of t (empty ones share their start with the
+// next), or -1 in front of the first and behind the last.
+__device__ __forceinline__ int request_of(const int32_t *q_start, int B, int t)
+{
+    int lo = 0, hi = B + 1;                      // number of starts <= t lies in [lo, hi]
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (q_start[mid] <= t) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo >= 1 && lo <= B ? lo - 1 : -1;
+}
+
+// A request as the kernels see it, its numbers brought into range whatever the arrays hold.
+struct Request {
+    int first, rows;                             // packed rows [first, first + rows), 0 <= first, first + rows <= T
+    int n, pos0, prefix;                         // tokens, position of its first row (may be negative), visible prefix (<= n)
+};
+__device__ __forceinline__ Request make_request(const int32_t *q_start, const int32_t *seq_len, const int32_t *prefix_len, int b, int T, int capacity)
+{
+    Request r;
+    const int lo = min(max(q_start[b], 0), T), hi = min(max(q_start[b + 1], 0), T);
+    r.first = lo;
+    r.rows = max(hi - lo, 0);
+    r.n = seq_len != nullptr ? min(max(seq_len[b], 0), capacity) : r.rows;
+    r.pos0 = r.n - r.rows;
+    r.prefix = prefix_len != nullptr ? min(max(prefix_len[b], 0), r.n) : 0;
+    return r;
+}
+
+}  // namespace lca
