@@ -1,0 +1,471 @@
+// Attention of a few rows per request over the paged 8-bit cache (include/lca_serve.h): single tokens, speculative ones.
+// Up to 16 NCT (row, query head) pairs of a KV head are the columns of 16x16x32 MFMAs:
+//   S^T[key, column] = K Q^T     A = keys,   B = the queries, in registers throughout
+//   O^T[dv, column] += V^T P^T   A = values, B = P^T = exp2(S^T - m)
+// Bound by reading the codes, once per request and KV head.  They go from memory straight into the registers that the
+// products read, without LDS, a barrier or a transpose, because the cache is laid out for it and the products' inner
+// index may be counted in any order that both operands agree on:
+//   keys    a lane takes 16 columns of a key in one load: the halves are its 8 elements of two k-steps, and the queries
+//           are loaded in that order;
+//   values  sixteen tokens of a column lie next to each other: a lane's 16 bytes are its 8 keys of two k-steps;
+//   P^T     row 4 q + r of S^T's block t (of four) is key 16 q + 4 t + r of the 64, so that a lane's sixteen weights
+//           are those of the sixteen tokens whose values it holds.
+// A code becomes a 16-bit element with the block's scale in one conversion of two (exact: powers of two).
+// A wavefront takes every fourth tile of 64 keys of its workgroup's part on its own; the loads of its next tile are
+// issued as soon as the registers of this one are free.  Softmax with a running maximum, sums in fp32 of the
+// weights before they are rounded.  Parts of long requests are joined by page_merge_kernel.
+#include <algorithm>
+
+#include "serve_row.h"
+
+namespace lca {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ floatx4 mfma_16x16x32(bf16x8 a, bf16x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ floatx4 mfma_16x16x32(f16x8 a, f16x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+template <typename E> struct Store;                        // the row code's tag of the element type
+template <> struct Store<__bf16> { typedef uint16_t type; };
+template <> struct Store<_Float16> { typedef f16_t type; };
+
+// Eight codes times a power of two as eight elements.
+template <typename E> __device__ __forceinline__ unsigned convert2(unsigned w, float scale, bool high);
+template <> __device__ __forceinline__ unsigned convert2<__bf16>(unsigned w, float scale, bool high)
+{
+    return high ? __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true))
+                : __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false));
+}
+template <> __device__ __forceinline__ unsigned convert2<_Float16>(unsigned w, float scale, bool high)
+{
+    return high ? __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, true))
+                : __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, false));
+}
+template <typename E> __device__ __forceinline__ auto convert8(unsigned lo, unsigned hi, float scale)
+{
+    typedef E ex8 __attribute__((ext_vector_type(8)));
+    const uint4 v = make_uint4(convert2<E>(lo, scale, false), convert2<E>(lo, scale, true), convert2<E>(hi, scale, false), convert2<E>(hi, scale, true));
+    return __builtin_bit_cast(ex8, v);
+}
+
+struct DecodeParams {
+    const void *q;
+    void *O;
+    float *lse, *part;
+    const int32_t *q_start, *seq_len, *prefix_len, *block_table;
+    const float *slopes;
+    const uint8_t *sel_q8, *pool_q8;
+    const float *scales;
+    ServeDims d;
+    ScoreRule rule;
+    int parts, per_part;                  // workgroups of a (request, KV head, group of columns); least tiles of one
+    int groups;                           // groups of 16 NCT columns
+    int most;                             // requests of more columns are left to the chunk kernel (INT_MAX: none)
+};
+
+constexpr int TILE = 64;
+
+// What a request's rows see, in tiles: [0, pre) and [from, to), numbered one behind the other.
+struct Tiles { int pre, from, count; };
+__device__ __forceinline__ Tiles make_tiles(const Request &r, int window)
+{
+    Tiles t;
+    const int first = max(r.pos0, 0);                                          // first row's position
+    const int lo = first >= window ? first - window + 1 : 0;                   // first key any row sees by the window
+    const int end = (r.n + TILE - 1) / TILE;
+    t.pre = min((r.prefix + TILE - 1) / TILE, end);
+    t.from = max(t.pre, lo / TILE);
+    t.count = t.pre + max(end - t.from, 0);
+    return t;
+}
+
+// A column's merged output: lanes hold V values each (columns lane * V ..) and the softmax's sum and maximum (base 2).  One that is not
+// finite is computed again over what its row sees alone (serve_row.h).
+template <typename E, int DV>
+__device__ __forceinline__ void finish_column(const DecodeParams &kp, const Request &r, int b, int s, int column, const float (&sum)[DV / 64], float l, float m, int lane)
+{
+    typedef typename Store<E>::type T;
+    constexpr int V = DV / 64;
+    const ServeDims &d = kp.d;
+    const int row = column / d.hps, h = s * d.hps + (column - row * d.hps), t = r.first + row;
+    T *O = (T *)kp.O + ((size_t)t * d.H + h) * d.d_pool;
+    float *lse = kp.lse != nullptr ? kp.lse + (size_t)t * d.H + h : nullptr;
+    bool fine = true;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    float o[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        o[v] = sum[v] * inv;
+        fine = fine && fabsf(o[v]) < INFINITY;
+    }
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!fine) != 0, 0)) {
+        const PagedSource<T> src{kp.block_table + (size_t)b * d.max_blocks, kp.sel_q8, kp.pool_q8, kp.scales, d.page, d.n_blocks, d.S, s, d.d_sel, d.d_pool};
+        scored_row<T, V>(src, (const T *)kp.q + (size_t)t * d.q_row + (size_t)h * d.d_sel, r, r.pos0 + row, kp.slopes != nullptr ? kp.slopes[h] * LOG2E : 0.f, kp.rule,
+                         d.d_sel, d.d_pool, O, lse, lane);
+        return;
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        if (lane * V + v < d.d_pool) O[lane * V + v] = from_float<T>(o[v]);
+    if (lse != nullptr && lane == 0) *lse = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+template <typename E, int DK, int DV, int NCT>
+__global__ __launch_bounds__(256, 2) void page_decode_kernel(const DecodeParams kp)
+{
+    typedef E ex8 __attribute__((ext_vector_type(8)));
+    constexpr int NK = DK / 64, NV = DV / 16, ROW = DV + 4;
+    __shared__ __attribute__((aligned(16))) float outs[4][16][ROW];
+    __shared__ float stats[4][16][2];
+
+    const ServeDims &d = kp.d;
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, q4 = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int unit = blockIdx.x / kp.parts, part = blockIdx.x - unit * kp.parts;
+    const int pair = unit / kp.groups, group = unit - pair * kp.groups;
+    const int b = pair / d.S, s = pair - b * d.S;
+    const Request r = make_request(kp.q_start, kp.seq_len, kp.prefix_len, b, d.T, d.max_blocks * d.page);
+    const int columns = r.rows * d.hps;
+    if (columns == 0 || columns > kp.most) return;
+    const Tiles tiles = make_tiles(r, kp.rule.window);
+    // more columns than there are groups for (a hint that was too small): the first part takes them all, unsplit
+    const bool many = columns > kp.groups * 16 * NCT;
+    const int parts = many ? 1 : kp.parts;
+    if (part >= parts) return;
+    const int per = max(kp.per_part, (tiles.count + parts - 1) / parts);
+    const int lo = part * per, hi = many ? tiles.count : min(lo + per, tiles.count);
+    if (lo >= hi && part > 0) return;                                          // (nothing to see at all: part 0 writes it)
+    const bool whole = lo == 0 && hi == tiles.count;                           // this workgroup has the request to itself
+
+    const int32_t *table = kp.block_table + (size_t)b * d.max_blocks;
+    const int strips = d.page >> 4, strip_end = (r.n + 15) >> 4;               // strips of 16 tokens: of a block, of the request
+    const int chunks = d.d_sel >> 4, cols16 = d.d_pool >> 4;
+
+    for (int cg = group; cg * 16 * NCT < columns; cg += kp.groups) {
+        const int c0 = cg * 16 * NCT;
+        // the columns' rows and heads; the queries in the order of the keys' loads
+        int pos[NCT];
+        float slope[NCT];
+        ex8 qf[NCT][2 * NK];
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct) {
+            const int c = min(c0 + 16 * ct + col, columns - 1), row = c / d.hps, h = s * d.hps + (c - row * d.hps);
+            pos[ct] = r.pos0 + row;
+            slope[ct] = kp.slopes != nullptr ? kp.slopes[h] * LOG2E : 0.f;
+            const E *qp = (const E *)kp.q + (size_t)(r.first + row) * d.q_row + (size_t)h * d.d_sel;
+#pragma unroll
+            for (int k = 0; k < NK; ++k)
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf)
+                    qf[ct][2 * k + hf] = q4 + 4 * k < chunks ? *reinterpret_cast<const ex8 *>(qp + 16 * (q4 + 4 * k) + 8 * hf) : ex8{0, 0, 0, 0, 0, 0, 0, 0};
+        }
+        floatx4 acc[NCT][NV];
+        float m_run[NCT], l_run[NCT];
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct) {
+            m_run[ct] = -INFINITY;
+            l_run[ct] = 0.f;
+#pragma unroll
+            for (int v = 0; v < NV; ++v) acc[ct][v] = floatx4{0.f, 0.f, 0.f, 0.f};
+        }
+
+        auto tile_at = [&](int x) { return x < tiles.pre ? x : x - tiles.pre + tiles.from; };
+        // the blocks of a lane's two strips of tile x: the one its key rows lie in, the one of its values; -1: none
+        auto block_of = [&](int strip) {
+            const int blk = table[min(strip, strip_end - 1) / strips];
+            return strip < strip_end && (unsigned)blk < (unsigned)d.n_blocks ? blk : -1;
+        };
+        uint4 kreg[4][NK], vreg[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) vreg[v] = make_uint4(0, 0, 0, 0);        // (columns behind d_pool stay so)
+        float k_scale = 1.f, v_scale = 1.f;
+        int k_blk = -1, v_blk = -1, k_next = -1, v_next = -1;
+        auto fetch_blocks = [&](int x) {
+            const int strip = 4 * tile_at(x);
+            k_next = block_of(strip + (col >> 2));
+            v_next = block_of(strip + q4);
+        };
+        auto load_keys = [&](int x) {
+            const int strip = 4 * tile_at(x) + (col >> 2);
+            k_blk = k_next;
+            const size_t u = (size_t)max(k_blk, 0) * d.S + s;
+            const uint8_t *p = kp.sel_q8 + (u * d.page + (strip % strips) * 16 + (col & 3)) * d.d_sel + 16 * q4;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int k = 0; k < NK; ++k)
+                    kreg[t][k] = q4 + 4 * k < chunks ? *reinterpret_cast<const uint4 *>(p + (size_t)4 * t * d.d_sel + 64 * k) : make_uint4(0, 0, 0, 0);
+            k_scale = kp.scales[2 * u + 1];
+        };
+        auto load_values = [&](int x) {
+            const int strip = 4 * tile_at(x) + q4;
+            v_blk = v_next;
+            const size_t u = (size_t)max(v_blk, 0) * d.S + s;
+            const uint8_t *p = kp.pool_q8 + ((u * strips + strip % strips) * d.d_pool + col) * 16;
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+                if (v < cols16) vreg[v] = *reinterpret_cast<const uint4 *>(p + 256 * v);
+            v_scale = kp.scales[2 * u];
+        };
+
+        const int pos_lo = max(r.pos0, 0), pos_hi = r.n - 1;                   // of the request's rows
+        int x = lo + wave;
+        if (x < hi) {
+            fetch_blocks(x);
+            load_keys(x);
+            load_values(x);
+            if (x + 4 < hi) fetch_blocks(x + 4);
+        }
+        for (; x < hi; x += 4) {
+            const int j0 = tile_at(x) * TILE + 16 * q4;                        // first key of the lane's strip
+            const int blk = v_blk;                                            // (its scores are those of the strip whose values it holds)
+            // S^T
+            floatx4 sacc[NCT][4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                ex8 kf[2 * NK];
+#pragma unroll
+                for (int k = 0; k < NK; ++k) {
+                    kf[2 * k] = convert8<E>(kreg[t][k].x, kreg[t][k].y, k_scale);
+                    kf[2 * k + 1] = convert8<E>(kreg[t][k].z, kreg[t][k].w, k_scale);
+                }
+#pragma unroll
+                for (int ct = 0; ct < NCT; ++ct) {
+                    sacc[ct][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int k = 0; k < 2 * NK; ++k) sacc[ct][t] = mfma_16x16x32(kf[k], qf[ct][k], sacc[ct][t]);
+                }
+            }
+            if (x + 4 < hi) load_keys(x + 4);
+
+            // does every row see the whole tile?
+            const int j_lo = tile_at(x) * TILE, j_hi = j_lo + TILE - 1;
+            const bool inside = j_hi <= pos_lo && (j_hi < r.prefix || pos_hi - j_lo < kp.rule.window);
+            const bool full = inside && __builtin_amdgcn_ballot_w64(blk < 0) == 0;
+            ex8 pb[NCT][2];
+#pragma unroll
+            for (int ct = 0; ct < NCT; ++ct) {
+                float lg[16], mx = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) lg[i] = sacc[ct][i >> 2][i & 3];
+                if (kp.rule.cap_log2 > 0.f) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) lg[i] = capped<true>(lg[i], kp.rule);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) lg[i] = capped<false>(lg[i], kp.rule);
+                }
+                if (kp.slopes != nullptr) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) lg[i] = fmaf(-slope[ct], fabsf((float)(pos[ct] - j0 - i)), lg[i]);
+                }
+                if (!full) {
+                    const int p = pos[ct];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int j = j0 + i;
+                        const bool seen = blk >= 0 && p >= 0 && j < r.n && ((j <= p && p - j < kp.rule.window) || j < r.prefix);
+                        lg[i] = seen ? lg[i] : -INFINITY;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, lg[i]);
+                mx = fmaxf(m_run[ct], lanes::across32(lanes::across16(mx, lanes::Max()), lanes::Max()));
+                if (__builtin_amdgcn_ballot_w64(mx > m_run[ct]) != 0) {
+                    const float f = mx == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[ct] - mx);
+                    m_run[ct] = mx;
+                    l_run[ct] *= f;
+#pragma unroll
+                    for (int v = 0; v < NV; ++v)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[ct][v][i] *= f;
+                }
+                const float ref = m_run[ct] == -INFINITY ? 0.f : m_run[ct];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float p = __builtin_amdgcn_exp2f(lg[i] - ref);
+                    l_run[ct] += p;
+                    pb[ct][i >> 3][i & 7] = (E)p;
+                }
+            }
+            // values that no row sees do not enter, whatever they are
+            if (!full) {
+                const int lo_all = pos_lo >= kp.rule.window ? pos_lo - kp.rule.window + 1 : 0;
+                unsigned keep[4];
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    keep[w] = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int j = j0 + 4 * w + i;
+                        if (blk >= 0 && j < r.n && (j >= lo_all || j < r.prefix)) keep[w] |= 0xFFu << (8 * i);
+                    }
+                }
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    vreg[v].x &= keep[0]; vreg[v].y &= keep[1]; vreg[v].z &= keep[2]; vreg[v].w &= keep[3];
+                }
+            }
+            // O^T
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const ex8 v0 = convert8<E>(vreg[v].x, vreg[v].y, v_scale), v1 = convert8<E>(vreg[v].z, vreg[v].w, v_scale);
+#pragma unroll
+                for (int ct = 0; ct < NCT; ++ct) {
+                    acc[ct][v] = mfma_16x16x32(v0, pb[ct][0], acc[ct][v]);
+                    acc[ct][v] = mfma_16x16x32(v1, pb[ct][1], acc[ct][v]);
+                }
+            }
+            if (x + 4 < hi) load_values(x + 4);
+            if (x + 8 < hi) fetch_blocks(x + 8);
+        }
+
+        // the four wavefronts' results, 16 columns at a time
+        for (int ct = 0; ct < NCT; ++ct) {
+            if (c0 + 16 * ct >= columns) break;
+            float m_ct = 0.f, l_ct = 0.f;
+#pragma unroll
+            for (int k = 0; k < NCT; ++k)
+                if (k == ct) {
+#pragma unroll
+                    for (int v = 0; v < NV; ++v) *reinterpret_cast<floatx4 *>(&outs[wave][col][16 * v + 4 * q4]) = acc[k][v];
+                    m_ct = m_run[k];
+                    l_ct = l_run[k];
+                }
+            l_ct = lanes::across32(lanes::across16(l_ct, lanes::Sum()), lanes::Sum());
+            if (q4 == 0) { stats[wave][col][0] = m_ct; stats[wave][col][1] = l_ct; }
+            __syncthreads();
+            for (int k = wave; k < 16 && c0 + 16 * ct + k < columns; k += 4) {
+                float m = -INFINITY, l = 0.f, sum[DV / 64], f[4];
+#pragma unroll
+                for (int w = 0; w < 4; ++w) m = fmaxf(m, stats[w][k][0]);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    f[w] = stats[w][k][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stats[w][k][0] - m);
+                    l += stats[w][k][1] * f[w];
+                }
+#pragma unroll
+                for (int v = 0; v < DV / 64; ++v) {
+                    sum[v] = 0.f;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) sum[v] = fmaf(outs[w][k][lane * (DV / 64) + v], f[w], sum[v]);
+                }
+                if (whole) {
+                    finish_column<E, DV>(kp, r, b, s, c0 + 16 * ct + k, sum, l, m, lane);
+                } else {
+                    float *dst = kp.part + (((size_t)unit * kp.parts + part) * 16 * NCT + 16 * ct + k) * (DV + 2);
+#pragma unroll
+                    for (int v = 0; v < DV / 64; ++v) dst[2 + lane * (DV / 64) + v] = sum[v];
+                    if (lane == 0) { dst[0] = m; dst[1] = l; }
+                }
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// Joins the parts of every column that has more than one: one wavefront per column.
+template <typename E, int DV>
+__global__ __launch_bounds__(256) void page_merge_kernel(const DecodeParams kp, int columns_per_unit)
+{
+    constexpr int V = DV / 64;
+    const ServeDims &d = kp.d;
+    const int lane = threadIdx.x & 63;
+    const long c = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int unit = (int)(c / columns_per_unit), k = (int)(c - (long)unit * columns_per_unit);
+    const int pair = unit / kp.groups, group = unit - pair * kp.groups, b = pair / d.S, s = pair - b * d.S;
+    if (b >= d.B) return;
+    const Request r = make_request(kp.q_start, kp.seq_len, kp.prefix_len, b, d.T, d.max_blocks * d.page);
+    const int columns = r.rows * d.hps, column = group * columns_per_unit + k;
+    if (column >= columns || columns > kp.most || columns > kp.groups * columns_per_unit) return;
+    const Tiles tiles = make_tiles(r, kp.rule.window);
+    const int per = max(kp.per_part, (tiles.count + kp.parts - 1) / kp.parts);
+    if (tiles.count <= per) return;                                            // one part: it has written the output
+    const int parts = (tiles.count + per - 1) / per;
+    const float *src = kp.part + ((size_t)unit * kp.parts * columns_per_unit + k) * (DV + 2);
+    const size_t step = (size_t)columns_per_unit * (DV + 2);
+    float m = -INFINITY, l = 0.f, sum[V];
+    for (int p = lane; p < parts; p += 64) m = fmaxf(m, src[p * step]);
+    m = lanes::over_group<64>(m, lanes::Max());
+#pragma unroll
+    for (int v = 0; v < V; ++v) sum[v] = 0.f;
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) {
+        const float *x = src + p * step;
+        const float f = x[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[0] - m);
+        l = fmaf(x[1], f, l);
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] = fmaf(x[2 + lane * V + v], f, sum[v]);
+    }
+    finish_column<E, DV>(kp, r, b, s, column, sum, l, m, lane);
+}
+
+struct Plan { int nct, groups, parts, per_part; };
+
+// How a call is split, from its sizes and hints.
+Plan make_plan(const ServeDims &d)
+{
+    Plan p;
+    const int dv = d.d_pool <= 64 && d.d_sel <= 64 ? 64 : d.d_pool <= 128 && d.d_sel <= 192 ? 128 : 256;
+    const int columns = (int)std::min<long>((long)d.max_q * d.hps, PAGE_DECODE_COLUMNS);
+    const int most = dv == 64 ? 4 : dv == 128 ? 2 : 1;                // (what the registers hold)
+    p.nct = columns <= 16 ? 1 : columns <= 32 ? 2 : 4;
+    if (p.nct > most) p.nct = most;
+    p.groups = (columns + 16 * p.nct - 1) / (16 * p.nct);
+    long keys = d.max_kv;
+    if (d.window > 0) keys = std::min<long>(keys, (long)d.window + d.max_q + TILE);
+    const long tiles = std::max<long>(1, (keys + TILE - 1) / TILE), units = (long)d.B * d.S * p.groups;
+    long parts = std::max<long>(1, 1024 / units);
+    parts = std::min<long>(parts, (tiles + 3) / 4);
+    p.per_part = (int)((tiles + parts - 1) / parts);
+    p.parts = (int)((tiles + p.per_part - 1) / p.per_part);
+    return p;
+}
+
+template <typename E, int DK, int DV> void run(const DecodeParams &kp, const Plan &p, hipStream_t st)
+{
+    const ServeDims &d = kp.d;
+    const unsigned grid = (unsigned)((long)d.B * d.S * p.groups * p.parts);
+    if constexpr (DV == 64)
+        if (p.nct == 4) page_decode_kernel<E, DK, DV, 4><<<grid, 256, 0, st>>>(kp);
+    if constexpr (DV <= 128)
+        if (p.nct == 2) page_decode_kernel<E, DK, DV, 2><<<grid, 256, 0, st>>>(kp);
+    if (p.nct == 1) page_decode_kernel<E, DK, DV, 1><<<grid, 256, 0, st>>>(kp);
+    if (p.parts > 1) {
+        const long columns = (long)d.B * d.S * p.groups * 16 * p.nct;
+        page_merge_kernel<E, DV><<<(unsigned)((columns + 3) / 4), 256, 0, st>>>(kp, 16 * p.nct);
+    }
+}
+
+template <typename E> void run_widths(const DecodeParams &kp, const Plan &p, hipStream_t st)
+{
+    const int dk = kp.d.d_sel, dv = kp.d.d_pool;
+    if (dk <= 64 && dv <= 64) run<E, 64, 64>(kp, p, st);
+    else if (dk <= 128 && dv <= 128) run<E, 128, 128>(kp, p, st);
+    else if (dk <= 192 && dv <= 128) run<E, 192, 128>(kp, p, st);
+    else run<E, 256, 256>(kp, p, st);
+}
+
+}  // namespace
+
+size_t page_decode_workspace_bytes(const ServeDims &d)
+{
+    const Plan p = make_plan(d);
+    const int dv = d.d_pool <= 64 && d.d_sel <= 64 ? 64 : d.d_pool <= 128 && d.d_sel <= 192 ? 128 : 256;
+    return p.parts > 1 ? (size_t)d.B * d.S * p.groups * p.parts * 16 * p.nct * (dv + 2) * sizeof(float) : 0;
+}
+
+hipError_t launch_page_decode(const ScoredArgs &a, int most, hipStream_t st)
+{
+    const Plan p = make_plan(a.d);
+    const DecodeParams kp{a.Q, a.O, a.lse, a.part, a.q_start, a.seq_len, a.prefix_len, a.block_table, a.slopes, a.sel_q8, a.pool_q8, a.scales, a.d, score_rule(a.d),
+                          p.parts, p.per_part, p.groups, most};
+    if (a.d.dtype == LCA_F16) run_widths<_Float16>(kp, p, st);
+    else run_widths<__bf16>(kp, p, st);
+    return hipGetLastError();
+}
+
+}  // namespace lca

@@ -1,5 +1,7 @@
 // Entry points of the serving operators (include/lca_serve.h): argument validation, workspace carving, dispatch.  The rules of
 // lca_api.hip hold here too: no allocation, no synchronisation, no state beyond the thread's error message.
+#include <algorithm>
+#include <climits>
 #include <cmath>
 
 #include "api_checks.h"
@@ -56,7 +58,7 @@ lca_status make_dims(const lca_serve_desc *desc, int what, ServeDims &d)
         if (desc->d_pool % 16 || desc->d_sel % 16 || desc->d_pool > 256 || desc->d_sel > 256)
             return fail(LCA_ERR_UNSUPPORTED, "the 8-bit cache takes widths that are multiples of 16 up to 256");
     }
-    const int capacity = what & CACHE ? desc->max_blocks * desc->page : desc->T;
+    const int capacity = (int)std::min<int64_t>(std::max<int64_t>((int64_t)desc->max_blocks * desc->page, 0), 1 << 30);
     d.max_q = desc->max_q == 0 || desc->max_q > desc->T ? desc->T : desc->max_q;
     d.max_kv = desc->max_kv == 0 || desc->max_kv > capacity ? capacity : desc->max_kv;
     return LCA_OK;
@@ -64,6 +66,9 @@ lca_status make_dims(const lca_serve_desc *desc, int what, ServeDims &d)
 
 size_t round_up(size_t n) { return (n + 255) & ~(size_t)255; }
 
+bool cache_widths(const ServeDims &d) { return d.dtype != LCA_F32 && d.d_pool % 16 == 0 && d.d_sel % 16 == 0 && d.d_pool <= 256 && d.d_sel <= 256; }
+// (a descriptor without a block table is no call over the cache: its fields need not make sense for one)
+size_t attn_bytes(const ServeDims &d) { return cache_widths(d) && d.T > 0 && d.max_blocks > 0 ? round_up(lca::page_decode_workspace_bytes(d)) : 0; }
 size_t tables_bytes(const ServeDims &d) { return round_up((size_t)d.B * sizeof(int32_t)); }
 
 lca_status check_i32(const void *p, const char *name, bool required = true)
@@ -91,7 +96,7 @@ lca_status lca_serve_workspace_size(const lca_serve_desc *desc, size_t *bytes)
     ServeDims d;
     LCA_TRY(make_dims(desc, 0, d));
     if (bytes == nullptr) return fail(LCA_ERR_INVALID_ARG, "bytes is NULL");
-    *bytes = tables_bytes(d);
+    *bytes = std::max(tables_bytes(d), attn_bytes(d));
     return LCA_OK;
 }
 
@@ -166,10 +171,11 @@ lca_status lca_page_attn_q8(const lca_serve_desc *desc, const void *q, const int
     LCA_TRY(check_ptr(O, "O", d.T > 0));
     LCA_TRY(check_i32(lse, "lse", false));
     if (d.T == 0) return LCA_OK;
+    LCA_TRY(check_ws(attn_bytes(d), workspace, workspace_bytes));
     lca::ScoredArgs a{};
     a.d = d; a.Q = q; a.q_start = q_start; a.seq_len = seq_len; a.prefix_len = prefix_len; a.slopes = slopes; a.block_table = block_table;
     a.sel_q8 = sel_q8; a.pool_q8 = pool_q8; a.scales = scales; a.O = O; a.lse = lse; a.part = static_cast<float *>(workspace);
-    return LCA_LAUNCH(lca::launch_scored_rows(a, static_cast<hipStream_t>(stream)), "lca_page_attn_q8");
+    return LCA_LAUNCH(lca::launch_page_decode(a, INT_MAX, static_cast<hipStream_t>(stream)), "lca_page_attn_q8");
 }
 
 lca_status lca_packed_attn(const lca_serve_desc *desc, const void *Q, const void *SEL, const void *POOL, const int32_t *doc_start,

@@ -53,6 +53,12 @@ struct ScoredArgs {
 };
 hipError_t launch_scored_rows(const ScoredArgs &a, hipStream_t st);
 
+// Requests of up to this many (row, query head) pairs per KV head are split over their keys (page_decode.hip).
+constexpr int PAGE_DECODE_COLUMNS = 64;
+size_t page_decode_workspace_bytes(const ServeDims &d);
+// Requests of at most `most` pairs (the others are left alone).
+hipError_t launch_page_decode(const ScoredArgs &a, int most, hipStream_t st);
+
 // ---- device functions ----
 
 constexpr float LOG2E = 1.4426950408889634f;
