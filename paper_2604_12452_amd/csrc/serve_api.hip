@@ -175,7 +175,12 @@ lca_status lca_page_attn_q8(const lca_serve_desc *desc, const void *q, const int
     lca::ScoredArgs a{};
     a.d = d; a.Q = q; a.q_start = q_start; a.seq_len = seq_len; a.prefix_len = prefix_len; a.slopes = slopes; a.block_table = block_table;
     a.sel_q8 = sel_q8; a.pool_q8 = pool_q8; a.scales = scales; a.O = O; a.lse = lse; a.part = static_cast<float *>(workspace);
-    return LCA_LAUNCH(lca::launch_page_decode(a, INT_MAX, static_cast<hipStream_t>(stream)), "lca_page_attn_q8");
+    // Requests of few rows are split over their keys, those of many share tiles in LDS.  Where the hint says that there are none of the
+    // second kind only the first kernel runs, and takes what comes.
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const bool long_ones = (long long)d.max_q * d.hps > lca::PAGE_DECODE_COLUMNS;
+    LCA_TRY(LCA_LAUNCH(lca::launch_page_decode(a, long_ones ? lca::PAGE_DECODE_COLUMNS : INT_MAX, st), "lca_page_attn_q8"));
+    return long_ones ? LCA_LAUNCH(lca::launch_scored_tile(a, lca::PAGE_DECODE_COLUMNS + 1, st), "lca_page_attn_q8") : LCA_OK;
 }
 
 lca_status lca_packed_attn(const lca_serve_desc *desc, const void *Q, const void *SEL, const void *POOL, const int32_t *doc_start,
@@ -195,7 +200,9 @@ lca_status lca_packed_attn(const lca_serve_desc *desc, const void *Q, const void
     lca::ScoredArgs a{};
     a.d = d; a.Q = Q; a.SEL = SEL; a.POOL = POOL; a.q_start = doc_start; a.prefix_len = prefix_len; a.slopes = slopes; a.O = O; a.lse = lse;
     a.part = static_cast<float *>(workspace);
-    return LCA_LAUNCH(lca::launch_scored_rows(a, static_cast<hipStream_t>(stream)), "lca_packed_attn");
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (lca::scored_tile_supported(d)) return LCA_LAUNCH(lca::launch_scored_tile(a, 0, st), "lca_packed_attn");
+    return LCA_LAUNCH(lca::launch_scored_rows(a, st), "lca_packed_attn");
 }
 
 }  // extern "C"

@@ -58,6 +58,9 @@ constexpr int PAGE_DECODE_COLUMNS = 64;
 size_t page_decode_workspace_bytes(const ServeDims &d);
 // Requests of at most `most` pairs (the others are left alone).
 hipError_t launch_page_decode(const ScoredArgs &a, int most, hipStream_t st);
+// Many rows, packed or over the cache: requests of at least `least` pairs (scored_tile.hip).
+bool scored_tile_supported(const ServeDims &d);
+hipError_t launch_scored_tile(const ScoredArgs &a, int least, hipStream_t st);
 
 // ---- device functions ----
 
