@@ -16,7 +16,7 @@
 
 #include <torch/csrc/autograd/python_variable.h>
 
-#include "lca.h"
+#include "lca_serve.h"
 
 namespace {
 
@@ -115,7 +115,7 @@ struct Call {
 enum Kind { ELT, I32, F32, U8, ANY };
 
 // Address of a tensor of at least `elems` elements of the kind asked for; false if lca.py has to look at it.
-bool address(PyObject *o, const Call &c, Kind kind, int64_t elems, bool optional, void *&out)
+bool address(PyObject *o, int32_t dtype, Kind kind, int64_t elems, bool optional, void *&out)
 {
     out = nullptr;
     if (o == Py_None) return optional || elems == 0;
@@ -125,7 +125,7 @@ bool address(PyObject *o, const Call &c, Kind kind, int64_t elems, bool optional
     const at::ScalarType s = t.scalar_type();
     switch (kind) {
     case ELT:
-        if (c.d.dtype == LCA_BF16 ? s != at::kBFloat16 && s != at::kShort && s != at::kUInt16 : s != (c.d.dtype == LCA_F32 ? at::kFloat : at::kHalf)) return false;
+        if (dtype == LCA_BF16 ? s != at::kBFloat16 && s != at::kShort && s != at::kUInt16 : s != (dtype == LCA_F32 ? at::kFloat : at::kHalf)) return false;
         break;
     case I32: if (s != at::kInt) return false; break;
     case F32: if (s != at::kFloat) return false; break;
@@ -137,6 +137,22 @@ bool address(PyObject *o, const Call &c, Kind kind, int64_t elems, bool optional
     return true;
 }
 
+// Address of a stream argument (asked for last: without a device there may be no stream to ask for).
+void *stream_address(PyObject *stream, bool &ok)
+{
+    if (!ok) return nullptr;
+    PyObject *v = PyObject_CallOneArg(stream_of, stream);
+    if (v == nullptr) return ok = missing(), nullptr;
+    void *p = PyLong_CheckExact(v) ? PyLong_AsVoidPtr(v) : nullptr;
+    ok = PyLong_CheckExact(v);
+    if (p == nullptr && PyErr_Occurred()) {             // (a number past any address)
+        ok = false;
+        PyErr_Clear();
+    }
+    Py_DECREF(v);
+    return p;
+}
+
 // Arguments one by one; `ok` goes false at the first that lca.py has to look at.
 struct Args {
     PyObject *const *o;
@@ -145,7 +161,7 @@ struct Args {
     void *take(Kind kind, Count elems, bool optional = false)
     {
         void *p = nullptr;
-        if (ok) ok = address(*o, c, kind, elems.v, optional, p);
+        if (ok) ok = address(*o, c.d.dtype, kind, elems.v, optional, p);
         ++o;
         return p;
     }
@@ -157,20 +173,7 @@ struct Args {
         else ok = false;
         return p;
     }
-    void *stream()
-    {
-        if (!ok) return nullptr;                 // (asked for last: without a device there may be no stream to ask for)
-        PyObject *v = PyObject_CallOneArg(stream_of, *o++);
-        if (v == nullptr) return ok = missing(), nullptr;
-        void *p = PyLong_CheckExact(v) ? PyLong_AsVoidPtr(v) : nullptr;
-        ok = PyLong_CheckExact(v);
-        if (p == nullptr && PyErr_Occurred()) {             // (a number past any address)
-            ok = false;
-            PyErr_Clear();
-        }
-        Py_DECREF(v);
-        return p;
-    }
+    void *stream() { return stream_address(*o++, ok); }
 };
 
 template <typename F> PyObject *run(F &&f)
@@ -328,6 +331,196 @@ PyObject *quantize_cache(PyObject *, PyObject *const *args, Py_ssize_t n)      /
     });
 }
 
+// ---- the calls of serve.py ----
+
+PyTypeObject *serve_type = nullptr;
+PyObject *device_of = nullptr;         // the current device's number
+enum ServeEntry { TABLES, RELEASE, STORE, PAGED, PACKED, N_SERVE };
+const char *const SERVE_NAMES[N_SERVE] = {"lca_page_tables", "lca_page_release", "lca_page_store_q8", "lca_page_attn_q8", "lca_packed_attn"};
+void *serve_entry[N_SERVE] = {};
+
+constexpr int N_SERVE_INTS = 13, N_ROWS = 3;
+const char *const SERVE_INTS[N_SERVE_INTS] = {"B", "T", "H", "S", "d_pool", "d_sel", "dtype", "page", "n_blocks", "max_blocks", "max_q", "max_kv", "window"};
+const char *const SERVE_FLOATS[2] = {"scale", "softcap"};
+const char *const SERVE_ROWS[N_ROWS] = {"q_row", "sel_row", "pool_row"};
+PyObject *serve_int_names[N_SERVE_INTS], *serve_float_names[2], *serve_row_names[N_ROWS];
+
+bool read_long(PyObject *o, PyObject *name, int64_t &out)
+{
+    PyObject *v = PyObject_GetAttr(o, name);
+    if (v == nullptr) return missing();
+    int overflow = 0;
+    const long x = PyLong_CheckExact(v) ? PyLong_AsLongAndOverflow(v, &overflow) : 0;
+    const bool ok = PyLong_CheckExact(v) && overflow == 0;
+    out = x;
+    Py_DECREF(v);
+    return ok;
+}
+
+// A call's descriptor and its arguments one by one; `ok` goes false at the first that serve.py has to look at.
+struct ServeArgs {
+    lca_serve_desc d;
+    PyObject *const *o;
+    int64_t device = -1;
+    bool ok = true;
+
+    ServeArgs(PyObject *const *args) : o(args + 1)
+    {
+        PyObject *desc = args[0];
+        int32_t *const ints[N_SERVE_INTS] = {&d.B, &d.T, &d.H, &d.S, &d.d_pool, &d.d_sel, &d.dtype, &d.page, &d.n_blocks, &d.max_blocks, &d.max_q, &d.max_kv, &d.window};
+        float *const floats[2] = {&d.scale, &d.softcap};
+        int64_t *const rows[N_ROWS] = {&d.q_row, &d.sel_row, &d.pool_row};
+        ok = Py_TYPE(desc) == serve_type;
+        for (int i = 0; i < N_SERVE_INTS && ok; ++i) ok = read_int(desc, serve_int_names[i], *ints[i]);
+        for (int i = 0; i < 2 && ok; ++i) ok = read_float(desc, serve_float_names[i], *floats[i]);
+        for (int i = 0; i < N_ROWS && ok; ++i) ok = read_long(desc, serve_row_names[i], *rows[i]);
+        ok = ok && d.B > 0 && d.T >= 0 && d.H > 0 && d.S > 0 && d.d_pool > 0 && d.d_sel > 0 && d.page >= 0 && d.n_blocks >= 0 && d.max_blocks >= 0;
+        ok = ok && (d.dtype == LCA_BF16 || d.dtype == LCA_F32 || d.dtype == LCA_F16);
+    }
+    void *take(Kind kind, Count elems, bool optional = false)
+    {
+        void *p = nullptr;
+        if (ok) ok = address(*o, d.dtype, kind, elems.v, optional, p);
+        if (ok && *o != Py_None) {               // all on one device
+            const int64_t here = THPVariable_Unpack(*o).get_device();
+            ok = device < 0 || device == here;
+            device = here;
+        }
+        ++o;
+        return p;
+    }
+    void *rows(int64_t heads, int64_t width, int64_t row)      // [T, heads, width], tokens `row` elements apart
+    {
+        const Count one = Count{heads} * width, before = Count{d.T - 1} * (row != 0 ? row : one.v);
+        int64_t elems = 0;
+        if (d.T > 0 && __builtin_add_overflow(before.v, one.v, &elems)) elems = INT64_MAX;
+        return take(ELT, Count{elems});
+    }
+    void *workspace(size_t &bytes)
+    {
+        PyObject *w = *o;
+        void *p = take(ANY, Count{0});
+        if (ok && w != Py_None) bytes = (size_t)THPVariable_Unpack(w).nbytes();
+        else ok = false;
+        return p;
+    }
+    void *stream()                               // ... which has to be the current one
+    {
+        if (!ok) return nullptr;
+        PyObject *v = PyObject_CallNoArgs(device_of);
+        if (v == nullptr) return ok = missing(), nullptr;
+        int overflow = 0;
+        ok = PyLong_CheckExact(v) && PyLong_AsLongAndOverflow(v, &overflow) == device && overflow == 0;
+        Py_DECREF(v);
+        return stream_address(*o++, ok);
+    }
+    Count B() const { return Count{d.B}; }
+    Count cache() const { return Count{d.n_blocks} * d.page * d.S; }
+};
+
+template <typename F> PyObject *guarded_serve(PyObject *const *args, Py_ssize_t n, Py_ssize_t want, F &&body)
+{
+    if (n != want || serve_type == nullptr) return pass();
+    try {
+        ServeArgs a(args);
+        return a.ok ? body(a, a.d) : pass();
+    } catch (...) {
+        return pass();
+    }
+}
+
+PyObject *page_tables(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded_serve(args, n, 14, [](ServeArgs &a, const lca_serve_desc &d) {
+        VP cached = a.take(I32, a.B()), added = a.take(I32, a.B()), list = a.take(I32, Count{d.n_blocks}), count = a.take(I32, Count{1}), left = a.take(I32, Count{1});
+        VP table = a.take(I32, a.B() * d.max_blocks), start = a.take(I32, Count{(int64_t)d.B + 1}), len = a.take(I32, a.B());
+        VP slot = a.take(I32, Count{d.T}), position = a.take(I32, Count{d.T}), request = a.take(I32, Count{d.T});
+        size_t bytes = 0;
+        VP ws = a.workspace(bytes), st = a.stream();
+        if (!a.ok) return pass();
+        return run([&] { return ((lca_status(*)(const lca_serve_desc *, CP, CP, CP, CP, VP, VP, VP, VP, VP, VP, VP, VP, size_t, VP))serve_entry[TABLES])(
+                                    &d, cached, added, list, count, left, table, start, len, slot, position, request, ws, bytes, st); });
+    });
+}
+
+PyObject *page_release(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded_serve(args, n, 7, [](ServeArgs &a, const lca_serve_desc &d) {
+        VP finished = a.take(I32, a.B()), cached = a.take(I32, a.B()), table = a.take(I32, a.B() * d.max_blocks), list = a.take(I32, Count{d.n_blocks}), count = a.take(I32, Count{1});
+        VP st = a.stream();
+        if (!a.ok) return pass();
+        return run([&] { return ((lca_status(*)(const lca_serve_desc *, CP, VP, VP, VP, VP, VP))serve_entry[RELEASE])(&d, finished, cached, table, list, count, st); });
+    });
+}
+
+PyObject *page_store_q8(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded_serve(args, n, 8, [](ServeArgs &a, const lca_serve_desc &d) {
+        VP sel = a.rows(d.S, d.d_sel, d.sel_row), pool = a.rows(d.S, d.d_pool, d.pool_row), slot = a.take(I32, Count{d.T});
+        VP sq = a.take(U8, a.cache() * d.d_sel), pq = a.take(U8, a.cache() * d.d_pool), sc = a.take(F32, Count{d.n_blocks} * d.S * 2), st = a.stream();
+        if (!a.ok) return pass();
+        return run([&] { return ((lca_status(*)(const lca_serve_desc *, CP, CP, CP, VP, VP, VP, VP))serve_entry[STORE])(&d, sel, pool, slot, sq, pq, sc, st); });
+    });
+}
+
+PyObject *page_attn_q8(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded_serve(args, n, 14, [](ServeArgs &a, const lca_serve_desc &d) {
+        VP q = a.rows(d.H, d.d_sel, d.q_row), start = a.take(I32, Count{(int64_t)d.B + 1}), len = a.take(I32, a.B()), prefix = a.take(I32, a.B(), true);
+        VP slopes = a.take(F32, Count{d.H}, true), table = a.take(I32, a.B() * d.max_blocks), sq = a.take(U8, a.cache() * d.d_sel), pq = a.take(U8, a.cache() * d.d_pool);
+        VP sc = a.take(F32, Count{d.n_blocks} * d.S * 2), O = a.take(ELT, Count{d.T} * d.H * d.d_pool), lse = a.take(F32, Count{d.T} * d.H, true);
+        size_t bytes = 0;
+        VP ws = a.workspace(bytes), st = a.stream();
+        if (!a.ok) return pass();
+        return run([&] { return ((lca_status(*)(const lca_serve_desc *, CP, CP, CP, CP, CP, CP, CP, CP, CP, VP, VP, VP, size_t, VP))serve_entry[PAGED])(
+                                    &d, q, start, len, prefix, slopes, table, sq, pq, sc, O, lse, ws, bytes, st); });
+    });
+}
+
+PyObject *packed_attn(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded_serve(args, n, 11, [](ServeArgs &a, const lca_serve_desc &d) {
+        VP Q = a.rows(d.H, d.d_sel, d.q_row), sel = a.rows(d.S, d.d_sel, d.sel_row), pool = a.rows(d.S, d.d_pool, d.pool_row);
+        VP start = a.take(I32, Count{(int64_t)d.B + 1}), prefix = a.take(I32, a.B(), true), slopes = a.take(F32, Count{d.H}, true);
+        VP O = a.take(ELT, Count{d.T} * d.H * d.d_pool), lse = a.take(F32, Count{d.T} * d.H, true);
+        size_t bytes = 0;
+        VP ws = a.workspace(bytes), st = a.stream();
+        if (!a.ok) return pass();
+        return run([&] { return ((lca_status(*)(const lca_serve_desc *, CP, CP, CP, CP, CP, CP, VP, VP, VP, size_t, VP))serve_entry[PACKED])(
+                                    &d, Q, sel, pool, start, prefix, slopes, O, lse, ws, bytes, st); });
+    });
+}
+
+// setup_serve(Desc, {entry point: address}, function for the current device's number), after setup.
+PyObject *setup_serve(PyObject *, PyObject *args)
+{
+    PyObject *dt, *addresses, *fn;
+    if (!PyArg_ParseTuple(args, "OO!O", &dt, &PyDict_Type, &addresses, &fn)) return nullptr;
+    if (stream_of == nullptr || !PyType_Check(dt) || !PyCallable_Check(fn)) {
+        PyErr_SetString(PyExc_TypeError, "setup_serve(Desc, addresses, function for the current device), after setup");
+        return nullptr;
+    }
+    void *found[N_SERVE];
+    for (int i = 0; i < N_SERVE; ++i) {
+        PyObject *v = PyDict_GetItemString(addresses, SERVE_NAMES[i]);
+        if (v == nullptr) {
+            PyErr_Format(PyExc_KeyError, "%s", SERVE_NAMES[i]);
+            return nullptr;
+        }
+        found[i] = PyLong_AsVoidPtr(v);
+        if (found[i] == nullptr) {
+            if (!PyErr_Occurred()) PyErr_Format(PyExc_ValueError, "%s has no address", SERVE_NAMES[i]);
+            return nullptr;
+        }
+    }
+    Py_INCREF(dt);
+    Py_INCREF(fn);
+    serve_type = (PyTypeObject *)dt;
+    device_of = fn;
+    for (int i = 0; i < N_SERVE; ++i) serve_entry[i] = found[i];
+    Py_RETURN_NONE;
+}
+
 // setup(Desc, CacheLayout, {entry point: address}, stream function, what is imported): torch's accessors are compiled in, so this module reads sizes and
 // addresses of tensors of the torch it was built for, and of no other's.
 PyObject *setup(PyObject *, PyObject *args)
@@ -369,6 +562,8 @@ PyObject *setup(PyObject *, PyObject *args)
 #define LCA_FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"setup", setup, METH_VARARGS, nullptr}, LCA_FAST(condense), LCA_FAST(prefill_attn), LCA_FAST(prefill_attn_up), LCA_FAST(dense_attn),
                          LCA_FAST(decode_attn), LCA_FAST(decode_attn_cached), LCA_FAST(decode_attn_q8), LCA_FAST(cache_update), LCA_FAST(quantize_cache),
+                         {"setup_serve", setup_serve, METH_VARARGS, nullptr}, LCA_FAST(page_tables), LCA_FAST(page_release), LCA_FAST(page_store_q8),
+                         LCA_FAST(page_attn_q8), LCA_FAST(packed_attn),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lcabind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -382,5 +577,11 @@ PyMODINIT_FUNC PyInit__lcabind()
         if ((float_names[i] = PyUnicode_InternFromString(FLOAT_FIELDS[i])) == nullptr) return nullptr;
     for (int i = 0; i < N_LAYOUT; ++i)
         if ((layout_names[i] = PyUnicode_InternFromString(LAYOUT_FIELDS[i])) == nullptr) return nullptr;
+    for (int i = 0; i < N_SERVE_INTS; ++i)
+        if ((serve_int_names[i] = PyUnicode_InternFromString(SERVE_INTS[i])) == nullptr) return nullptr;
+    for (int i = 0; i < 2; ++i)
+        if ((serve_float_names[i] = PyUnicode_InternFromString(SERVE_FLOATS[i])) == nullptr) return nullptr;
+    for (int i = 0; i < N_ROWS; ++i)
+        if ((serve_row_names[i] = PyUnicode_InternFromString(SERVE_ROWS[i])) == nullptr) return nullptr;
     return PyModule_Create(&module);
 }

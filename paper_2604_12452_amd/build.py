@@ -13,6 +13,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "liblca.so")
+HEADERS = [os.path.join(ROOT, "include", f) for f in ("lca.h", "lca_serve.h")]
 BIND_SRC = os.path.join(PKG, "binding", "bind.cpp")
 BIND = os.path.join(PKG, "_lcabind.so")       # the binding's marshalling in native code (lca.py does without where it does not load)
 
@@ -32,7 +33,7 @@ def sources():
 
 def _compile(src: str, force: bool) -> str:
     obj = os.path.join(OBJ, os.path.basename(src) + ".o")
-    deps = [src] + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")] + [os.path.join(ROOT, "include", f) for f in os.listdir(os.path.join(ROOT, "include"))]
+    deps = [src] + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")] + HEADERS
     if not force and os.path.exists(obj) and all(os.path.getmtime(obj) >= os.path.getmtime(d) for d in deps):
         return obj
     subprocess.run([HIPCC, *FLAGS, "-c", src, "-o", obj], check=True)
@@ -44,7 +45,7 @@ def _build_binding(force: bool) -> None:
     import torch
     from .lca import bind_tag
     tag = bind_tag()
-    if not force and os.path.exists(BIND) and all(os.path.getmtime(BIND) >= os.path.getmtime(d) for d in (BIND_SRC, os.path.join(ROOT, "include", "lca.h"))):
+    if not force and os.path.exists(BIND) and all(os.path.getmtime(BIND) >= os.path.getmtime(d) for d in (BIND_SRC, *HEADERS)):
         with open(BIND, "rb") as f:
             if tag.encode() + b"\0" in f.read():
                 return

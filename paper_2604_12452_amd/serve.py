@@ -1,5 +1,6 @@
 """Binding of the serving operators (include/lca_serve.h): ragged batches over a paged 8-bit cache, and packed prompts.  As in ``lca``:
-argument marshalling only, torch provides device memory and streams, every step runs in the library's HIP kernels.
+argument marshalling only (in native code, binding/bind.cpp, for plain descriptors and tensors, here for the others), torch provides device memory and
+streams, every step runs in the library's HIP kernels.
 """
 from __future__ import annotations
 
@@ -53,11 +54,12 @@ def _c_desc(*key):
 
 
 _lib = None
+_bind = None            # the native marshalling, as in lca.py
 
 
 def load() -> ctypes.CDLL:
     """The library, with these entry points' argument types declared."""
-    global _lib
+    global _lib, _bind
     if _lib is None:
         lib = lca.load()
         p, n = ctypes.c_void_p, ctypes.c_size_t
@@ -66,6 +68,11 @@ def load() -> ctypes.CDLL:
             f = getattr(lib, name)
             f.restype, f.argtypes = ctypes.c_int, args
         _lib = lib
+        if lca._bind is not None:
+            import torch
+            lca._bind.setup_serve(Desc, {name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in EXPORTS},
+                                   getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device))
+            _bind = lca._bind
     return _lib
 
 
@@ -131,6 +138,8 @@ def _call(name, desc, *args):
 
 
 def page_tables(desc: Desc, cached_len, new_len, free_list, free_count, free_left, block_table, q_start, seq_len, slot, position, request, workspace, stream=None):
+    if _bind is not None and lca._done(_bind.page_tables(desc, cached_len, new_len, free_list, free_count, free_left, block_table, q_start, seq_len, slot, position, request, workspace, stream)):
+        return
     B, T = desc.B, desc.T
     _fit(desc, "i32", (cached_len, "cached_len", B), (new_len, "new_len", B), (free_list, "free_list", desc.n_blocks), (free_count, "free_count", 1),
          (free_left, "free_left", 1), (block_table, "block_table", B * desc.max_blocks), (q_start, "q_start", B + 1), (seq_len, "seq_len", B), (slot, "slot", T),
@@ -141,6 +150,8 @@ def page_tables(desc: Desc, cached_len, new_len, free_list, free_count, free_lef
 
 
 def page_release(desc: Desc, finished, cached_len, block_table, free_list, free_count, stream=None):
+    if _bind is not None and lca._done(_bind.page_release(desc, finished, cached_len, block_table, free_list, free_count, stream)):
+        return
     _fit(desc, "i32", (finished, "finished", desc.B), (cached_len, "cached_len", desc.B), (block_table, "block_table", desc.B * desc.max_blocks),
          (free_list, "free_list", desc.n_blocks), (free_count, "free_count", 1))
     _same_device(cached_len=cached_len, block_table=block_table)
@@ -154,6 +165,8 @@ def _fit_cache(desc, sel_q8, pool_q8, scales):
 
 
 def page_store_q8(desc: Desc, SEL, POOL, slot, sel_q8, pool_q8, scales, stream=None):
+    if _bind is not None and lca._done(_bind.page_store_q8(desc, SEL, POOL, slot, sel_q8, pool_q8, scales, stream)):
+        return
     _fit_rows(desc, SEL, "SEL", desc.S, desc.d_sel, desc.sel_row)
     _fit_rows(desc, POOL, "POOL", desc.S, desc.d_pool, desc.pool_row)
     _fit(desc, "i32", (slot, "slot", desc.T))
@@ -169,6 +182,8 @@ def _fit_rule(desc, prefix_len, slopes, O, lse):
 
 
 def page_attn_q8(desc: Desc, q, q_start, seq_len, prefix_len, slopes, block_table, sel_q8, pool_q8, scales, O, lse, workspace, stream=None):
+    if _bind is not None and lca._done(_bind.page_attn_q8(desc, q, q_start, seq_len, prefix_len, slopes, block_table, sel_q8, pool_q8, scales, O, lse, workspace, stream)):
+        return
     _fit_rows(desc, q, "q", desc.H, desc.d_sel, desc.q_row)
     _fit(desc, "i32", (q_start, "q_start", desc.B + 1), (seq_len, "seq_len", desc.B), (block_table, "block_table", desc.B * desc.max_blocks))
     _fit_rule(desc, prefix_len, slopes, O, lse)
@@ -179,6 +194,8 @@ def page_attn_q8(desc: Desc, q, q_start, seq_len, prefix_len, slopes, block_tabl
 
 
 def packed_attn(desc: Desc, Q, SEL, POOL, doc_start, prefix_len, slopes, O, lse, workspace, stream=None):
+    if _bind is not None and lca._done(_bind.packed_attn(desc, Q, SEL, POOL, doc_start, prefix_len, slopes, O, lse, workspace, stream)):
+        return
     _fit_rows(desc, Q, "Q", desc.H, desc.d_sel, desc.q_row)
     _fit_rows(desc, SEL, "SEL", desc.S, desc.d_sel, desc.sel_row)
     _fit_rows(desc, POOL, "POOL", desc.S, desc.d_pool, desc.pool_row)
