@@ -66,9 +66,22 @@ lca_status make_dims(const lca_serve_desc *desc, int what, ServeDims &d)
 
 size_t round_up(size_t n) { return (n + 255) & ~(size_t)255; }
 
-bool cache_widths(const ServeDims &d) { return d.dtype != LCA_F32 && d.d_pool % 16 == 0 && d.d_sel % 16 == 0 && d.d_pool <= 256 && d.d_sel <= 256; }
-// (a descriptor without a block table is no call over the cache: its fields need not make sense for one)
-size_t attn_bytes(const ServeDims &d) { return cache_widths(d) && d.T > 0 && d.max_blocks > 0 ? round_up(lca::page_decode_workspace_bytes(d)) : 0; }
+// Requests of few rows are split over their keys, those of many share tiles in LDS.  Where the hint says that there are none
+// of the second kind only the first kernel runs, and takes what comes.
+bool long_requests(const ServeDims &d) { return (long long)d.max_q * d.hps > lca::PAGE_DECODE_COLUMNS; }
+
+size_t paged_bytes(const ServeDims &d)
+{
+    const size_t few = lca::page_decode_workspace_bytes(d), many = long_requests(d) ? lca::scored_tile_workspace_bytes(d, true) : 0;
+    return round_up(std::max(few, many));                // (one kernel after the other)
+}
+size_t packed_bytes(const ServeDims &d) { return d.T > 0 && lca::scored_tile_supported(d) ? round_up(lca::scored_tile_workspace_bytes(d, false)) : 0; }
+// (a descriptor that the cache calls refuse needs no workspace for them)
+size_t attn_bytes(const lca_serve_desc *desc)
+{
+    ServeDims d;
+    return make_dims(desc, CACHE, d) == LCA_OK && d.T > 0 ? paged_bytes(d) : 0;
+}
 size_t tables_bytes(const ServeDims &d) { return round_up((size_t)d.B * sizeof(int32_t)); }
 
 lca_status check_i32(const void *p, const char *name, bool required = true)
@@ -96,7 +109,7 @@ lca_status lca_serve_workspace_size(const lca_serve_desc *desc, size_t *bytes)
     ServeDims d;
     LCA_TRY(make_dims(desc, 0, d));
     if (bytes == nullptr) return fail(LCA_ERR_INVALID_ARG, "bytes is NULL");
-    *bytes = std::max(tables_bytes(d), attn_bytes(d));
+    *bytes = std::max({tables_bytes(d), packed_bytes(d), attn_bytes(desc)});
     return LCA_OK;
 }
 
@@ -171,16 +184,13 @@ lca_status lca_page_attn_q8(const lca_serve_desc *desc, const void *q, const int
     LCA_TRY(check_ptr(O, "O", d.T > 0));
     LCA_TRY(check_i32(lse, "lse", false));
     if (d.T == 0) return LCA_OK;
-    LCA_TRY(check_ws(attn_bytes(d), workspace, workspace_bytes));
+    LCA_TRY(check_ws(paged_bytes(d), workspace, workspace_bytes));
     lca::ScoredArgs a{};
     a.d = d; a.Q = q; a.q_start = q_start; a.seq_len = seq_len; a.prefix_len = prefix_len; a.slopes = slopes; a.block_table = block_table;
     a.sel_q8 = sel_q8; a.pool_q8 = pool_q8; a.scales = scales; a.O = O; a.lse = lse; a.part = static_cast<float *>(workspace);
-    // Requests of few rows are split over their keys, those of many share tiles in LDS.  Where the hint says that there are none of the
-    // second kind only the first kernel runs, and takes what comes.
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const bool long_ones = (long long)d.max_q * d.hps > lca::PAGE_DECODE_COLUMNS;
-    LCA_TRY(LCA_LAUNCH(lca::launch_page_decode(a, long_ones ? lca::PAGE_DECODE_COLUMNS : INT_MAX, st), "lca_page_attn_q8"));
-    return long_ones ? LCA_LAUNCH(lca::launch_scored_tile(a, lca::PAGE_DECODE_COLUMNS + 1, st), "lca_page_attn_q8") : LCA_OK;
+    LCA_TRY(LCA_LAUNCH(lca::launch_page_decode(a, long_requests(d) ? lca::PAGE_DECODE_COLUMNS : INT_MAX, st), "lca_page_attn_q8"));
+    return long_requests(d) ? LCA_LAUNCH(lca::launch_scored_tile_paged(a, lca::PAGE_DECODE_COLUMNS + 1, st), "lca_page_attn_q8") : LCA_OK;
 }
 
 lca_status lca_packed_attn(const lca_serve_desc *desc, const void *Q, const void *SEL, const void *POOL, const int32_t *doc_start,
@@ -197,11 +207,12 @@ lca_status lca_packed_attn(const lca_serve_desc *desc, const void *Q, const void
     LCA_TRY(check_ptr(O, "O", d.T > 0));
     LCA_TRY(check_i32(lse, "lse", false));
     if (d.T == 0) return LCA_OK;
+    LCA_TRY(check_ws(packed_bytes(d), workspace, workspace_bytes));
     lca::ScoredArgs a{};
     a.d = d; a.Q = Q; a.SEL = SEL; a.POOL = POOL; a.q_start = doc_start; a.prefix_len = prefix_len; a.slopes = slopes; a.O = O; a.lse = lse;
     a.part = static_cast<float *>(workspace);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (lca::scored_tile_supported(d)) return LCA_LAUNCH(lca::launch_scored_tile(a, 0, st), "lca_packed_attn");
+    if (lca::scored_tile_supported(d)) return LCA_LAUNCH(lca::launch_scored_tile(a, st), "lca_packed_attn");
     return LCA_LAUNCH(lca::launch_scored_rows(a, st), "lca_packed_attn");
 }
 

@@ -58,9 +58,11 @@ constexpr int PAGE_DECODE_COLUMNS = 64;
 size_t page_decode_workspace_bytes(const ServeDims &d);
 // Requests of at most `most` pairs (the others are left alone).
 hipError_t launch_page_decode(const ScoredArgs &a, int most, hipStream_t st);
-// Many rows, packed or over the cache: requests of at least `least` pairs (scored_tile.hip).
+// Many rows: packed prompts, and over the cache the requests of at least `least` pairs (scored_tile.h).
 bool scored_tile_supported(const ServeDims &d);
-hipError_t launch_scored_tile(const ScoredArgs &a, int least, hipStream_t st);
+size_t scored_tile_workspace_bytes(const ServeDims &d, bool paged);
+hipError_t launch_scored_tile(const ScoredArgs &a, hipStream_t st);
+hipError_t launch_scored_tile_paged(const ScoredArgs &a, int least, hipStream_t st);
 
 // ---- device functions ----
 
