@@ -419,7 +419,7 @@ Plan make_plan(const ServeDims &d)
     if (d.window > 0) keys = std::min<long>(keys, (long)d.window + d.max_q + TILE);
     const long tiles = std::max<long>(1, (keys + TILE - 1) / TILE), units = (long)d.B * d.S * p.groups;
     long parts = std::max<long>(1, 1024 / units);
-    parts = std::min<long>(parts, (tiles + 3) / 4);
+    parts = tiles <= 16 ? 1 : std::min<long>(parts, (tiles + 3) / 4);
     p.per_part = (int)((tiles + parts - 1) / parts);
     p.parts = (int)((tiles + p.per_part - 1) / p.per_part);
     return p;

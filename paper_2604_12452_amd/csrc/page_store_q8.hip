@@ -1,14 +1,14 @@
 // New keys and values into the paged 8-bit cache (include/lca_serve.h): one E4M3 code per element, one power-of-two scale
 // per block of tokens, KV head and component.
 //
-// Unit = the tokens of one block in this call, one KV head; one workgroup takes both components of it, so that nobody else
-// reads or writes its codes and scales.  Two passes over the unit's new values, largest magnitude, then codes: the second reads
-// what the first has brought into the caches.  A power-of-two scale makes x / scale exact, the only rounding is the
-// conversion's.  When the block's scale rises, the codes in front of the new tokens are converted again, old / new being a
-// power of two as well: exact but for codes that leave E4M3's normal range.
-// Values lie sixteen tokens of a column next to each other: a thread takes sixteen tokens of a pair of columns, reads them
-// four bytes at a time (a wavefront: 256 bytes of a row) and writes two whole 16-byte pieces; a piece that holds older
-// tokens, or places behind the new ones, is read first and keeps them.
+// Unit = the tokens of one block in this call, one KV head; one wavefront takes a component of it, so that nobody else reads or
+// writes its codes and scale, and nothing is shared but lanes.  The unit's new values are read once and held in registers
+// from the largest magnitude to the codes (up to 8192 of them, 64 tokens of 128; larger units are read twice).  A power-of-two
+// scale makes x / scale exact, the only rounding is the conversion's.  When the block's scale rises, the codes in front of the new
+// tokens are converted again, old / new being a power of two as well: exact but for codes that leave E4M3's normal range.
+// Keys: a lane takes sixteen columns of a token, 32 bytes in, 16 out.  Values lie sixteen tokens of a column next to each other: a lane
+// takes sixteen tokens of a pair of columns, reads them four bytes at a time (a wavefront: 256 bytes of a row) and writes two
+// whole 16-byte pieces; a piece that holds older tokens, or places behind the new ones, is read first and keeps them.
 // Bound by memory: two bytes read and one written per element.
 #include "serve_internal.h"
 
@@ -20,9 +20,13 @@ struct StoreParams {
     const int32_t *slot;
     uint8_t *sel_q8, *pool_q8;
     float *scales;
-    int T, S, d_pool, d_sel, page, n_blocks, window;       // window: packed rows a workgroup looks for starts of units in
+    int T, S, d_pool, d_sel, page, n_blocks, window;       // window: packed rows a wavefront looks for starts of units in
+    unsigned pieces_magic, pairs_magic;                    // for divisions by d_sel / 16 and d_pool / 2 (quotient)
     size_t sel_row, pool_row;
 };
+
+// x / d for x * d < 2^32, with magic = 2^32 / d + 1 (rounded down; d >= 2), or 0 for d = 1.
+__device__ __forceinline__ int quotient(int x, unsigned magic) { return magic == 0 ? x : (int)__umulhi((unsigned)x, magic); }
 
 template <typename T> struct Range;                      // exponents of a block's scale: the decoded codes stay finite numbers of the type
 template <> struct Range<uint16_t> { static constexpr int LO = -100, HI = 119; };
@@ -59,140 +63,201 @@ __device__ __forceinline__ unsigned recode4(unsigned w, float factor)
                    in_range(__builtin_amdgcn_cvt_f32_fp8((int)w, 2), factor), in_range(__builtin_amdgcn_cvt_f32_fp8((int)w, 3), factor));
 }
 
-template <typename T>
-__device__ __forceinline__ void store_unit(const StoreParams &kp, int t0, int block, int off, int n, int s, float (&maxima)[2][4], int tid)
+// The unit's scale and what becomes of the older codes.
+struct Scale { float value, inv, factor; bool raised; };
+template <typename T> __device__ __forceinline__ Scale new_scale(float amax, float old, int off)
 {
-    const int lane = tid & 63, wave = tid >> 6;
-    const size_t unit = (size_t)block * kp.S + s;
-    const uint16_t *sel = (const uint16_t *)kp.SEL + (size_t)t0 * kp.sel_row + (size_t)s * kp.d_sel;
-    const uint16_t *pool = (const uint16_t *)kp.POOL + (size_t)t0 * kp.pool_row + (size_t)s * kp.d_pool;
-    const float2 old = *reinterpret_cast<const float2 *>(kp.scales + 2 * unit);      // (pooled, selected)
-
-    // largest magnitudes (fmaxf drops a NaN)
-    auto largest = [&](const uint16_t *x, size_t row, int d) {
-        const int pieces = d / 8;
-        float m = 0.f;
-        for (int u = tid; u < n * pieces; u += 256) {
-            const int t = u / pieces, c = u - t * pieces;
-            const uint4 v = *reinterpret_cast<const uint4 *>(x + (size_t)t * row + 8 * c);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    const float fresh = ldexpf(1.f, scale_exponent<T>(lanes::over_group<64>(amax, lanes::Max())));
+    Scale c;
+    const bool keep = off > 0 && old >= fresh;
+    c.value = keep ? old : fresh;
+    c.inv = 1.f / c.value;
+    c.raised = off > 0 && !keep;
+    c.factor = old * c.inv;
+    return c;
+}
+template <typename T> __device__ __forceinline__ float largest8(const uint4 &v, float m)     // (fmaxf drops a NaN)
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = unpack2<T>(w[i]);
-                m = fmaxf(m, fmaxf(fabsf(f.x), fabsf(f.y)));
-            }
-        }
-        return lanes::over_group<64>(m, lanes::Max());
-    };
-    const float m_pool = largest(pool, kp.pool_row, kp.d_pool), m_sel = largest(sel, kp.sel_row, kp.d_sel);
-    __syncthreads();                                     // (the unit before is done with `maxima`; the scales have been read)
-    if (lane == 0) { maxima[0][wave] = m_pool; maxima[1][wave] = m_sel; }
-    __syncthreads();
-    float scale[2], inv[2], factor[2];
-    bool raised[2];
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        const float m = fmaxf(fmaxf(maxima[c][0], maxima[c][1]), fmaxf(maxima[c][2], maxima[c][3]));
-        const int e = scale_exponent<T>(m);
-        const float before = c == 0 ? old.x : old.y, fresh = ldexpf(1.f, e);
-        raised[c] = off > 0 && !(before >= fresh);
-        scale[c] = off > 0 && before >= fresh ? before : fresh;
-        inv[c] = 1.f / scale[c];
-        factor[c] = before * inv[c];
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = unpack2<T>(w[i]);
+        m = fmaxf(m, fmaxf(fabsf(f.x), fabsf(f.y)));
     }
-    if (tid == 0) *reinterpret_cast<float2 *>(kp.scales + 2 * unit) = float2{scale[0], scale[1]};
-
-    // keys: 16 codes at a time; older tokens only when the scale rose
-    {
-        const int pieces = kp.d_sel / 16, first = raised[1] ? 0 : off;
-        uint8_t *dst = kp.sel_q8 + unit * kp.page * kp.d_sel;
-        for (int u = tid; u < (off + n - first) * pieces; u += 256) {
-            const int at = u / pieces, c = u - at * pieces, token = first + at;
-            uint4 *p = reinterpret_cast<uint4 *>(dst + (size_t)token * kp.d_sel + 16 * c);
-            uint4 out;
-            if (token < off) {
-                const uint4 v = *p;
-                out = make_uint4(recode4(v.x, factor[1]), recode4(v.y, factor[1]), recode4(v.z, factor[1]), recode4(v.w, factor[1]));
-            } else {
-                const uint4 *x = reinterpret_cast<const uint4 *>(sel + (size_t)(token - off) * kp.sel_row + 16 * c);
-                const uint4 a = x[0], b = x[1];
-                const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-                uint32_t o[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 f = unpack2<T>(w[2 * i]), g = unpack2<T>(w[2 * i + 1]);
-                    o[i] = encode4(in_range(f.x, inv[1]), in_range(f.y, inv[1]), in_range(g.x, inv[1]), in_range(g.y, inv[1]));
-                }
-                out = make_uint4(o[0], o[1], o[2], o[3]);
-            }
-            *p = out;
-        }
-    }
-    // values: sixteen tokens of two columns at a time
-    {
-        const int pairs = kp.d_pool / 2, first = raised[0] ? 0 : off >> 4, last = (off + n - 1) >> 4;
-        uint8_t *dst = kp.pool_q8 + unit * kp.page * kp.d_pool;
-        for (int u = tid; u < (last - first + 1) * pairs; u += 256) {
-            const int at = u / pairs, c = u - at * pairs, strip = first + at;
-            uint4 *p = reinterpret_cast<uint4 *>(dst + ((size_t)strip * kp.d_pool + 2 * c) * 16);
-            const int lo = off - 16 * strip, hi = lo + n;       // the new tokens' places in the strip, cut to [0, 16)
-            unsigned o[2][4];
-            if (lo > 0 || hi < 16) {                            // some places keep what they hold, those of older tokens perhaps recoded
-                const uint4 v[2] = {p[0], p[1]};
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const unsigned w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        unsigned r = raised[0] ? recode4(w[i], factor[0]) : w[i];
-                        // places at and behind the first new one are not recoded
-                        const int keep = min(max(lo - 4 * i, 0), 4);
-                        const unsigned mask = keep == 4 ? 0xFFFFFFFFu : (1u << (8 * keep)) - 1;
-                        o[k][i] = (r & mask) | (w[i] & ~mask);
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[0][i] = o[1][i] = 0;
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float2 f[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int place = 4 * i + j;
-                    f[j] = float2{0.f, 0.f};
-                    if (place >= lo && place < hi) f[j] = unpack2<T>(*reinterpret_cast<const uint32_t *>(pool + (size_t)(place - lo) * kp.pool_row + 2 * c));
-                }
-                const int from = min(max(lo - 4 * i, 0), 4), to = min(max(hi - 4 * i, 0), 4);
-                const unsigned upto_to = to == 4 ? 0xFFFFFFFFu : (1u << (8 * to)) - 1, upto_from = from == 4 ? 0xFFFFFFFFu : (1u << (8 * from)) - 1;
-                const unsigned mask = upto_to & ~upto_from;     // bytes of the new tokens
-                const unsigned c0 = encode4(in_range(f[0].x, inv[0]), in_range(f[1].x, inv[0]), in_range(f[2].x, inv[0]), in_range(f[3].x, inv[0]));
-                const unsigned c1 = encode4(in_range(f[0].y, inv[0]), in_range(f[1].y, inv[0]), in_range(f[2].y, inv[0]), in_range(f[3].y, inv[0]));
-                o[0][i] = (o[0][i] & ~mask) | (c0 & mask);
-                o[1][i] = (o[1][i] & ~mask) | (c1 & mask);
-            }
-            p[0] = make_uint4(o[0][0], o[0][1], o[0][2], o[0][3]);
-            p[1] = make_uint4(o[1][0], o[1][1], o[1][2], o[1][3]);
-        }
-    }
+    return m;
+}
+template <typename T> __device__ __forceinline__ uint2 encode8(const uint4 &v, float inv)
+{
+    const float2 a = unpack2<T>(v.x), b = unpack2<T>(v.y), c = unpack2<T>(v.z), d = unpack2<T>(v.w);
+    return uint2{encode4(in_range(a.x, inv), in_range(a.y, inv), in_range(b.x, inv), in_range(b.y, inv)),
+                 encode4(in_range(c.x, inv), in_range(c.y, inv), in_range(d.x, inv), in_range(d.y, inv))};
 }
 
-// A workgroup takes the units that start among `window` packed rows, one KV head.  A unit starts where a token's slot does not
-// follow the slot of the token in front of it, or opens a block, and ends where either happens again.
+constexpr int K_HELD = 8, V_HELD = 4;                      // items of a lane that registers hold
+
+// Keys: item u = 16 columns of a new token.
+template <typename T> __device__ __forceinline__ void store_keys(const StoreParams &kp, int t0, int block, int off, int n, int s, int lane)
+{
+    const size_t unit = (size_t)block * kp.S + s;
+    const uint16_t *x = (const uint16_t *)kp.SEL + (size_t)t0 * kp.sel_row + (size_t)s * kp.d_sel;
+    uint8_t *dst = kp.sel_q8 + (unit * kp.page + off) * kp.d_sel;
+    float *scale = kp.scales + 2 * unit + 1;
+    const int pieces = kp.d_sel / 16, total = n * pieces;
+    const bool held = total <= 64 * K_HELD;
+    auto source = [&](int u) {
+        const int t = quotient(u, kp.pieces_magic);
+        return reinterpret_cast<const uint4 *>(x + (size_t)t * kp.sel_row + 16 * (u - t * pieces));
+    };
+    auto target = [&](int u) { return reinterpret_cast<uint4 *>(dst + 16 * (size_t)u); };      // (tokens of a block follow one another)
+    uint4 a[K_HELD], b[K_HELD];
+    float m = 0.f;
+    const float old = off > 0 ? *scale : 0.f;
+    if (held) {
+#pragma unroll
+        for (int i = 0; i < K_HELD; ++i) {
+            a[i] = b[i] = make_uint4(0, 0, 0, 0);
+            if (64 * i + lane < total) { const uint4 *p = source(64 * i + lane); a[i] = p[0]; b[i] = p[1]; }
+        }
+#pragma unroll
+        for (int i = 0; i < K_HELD; ++i) m = largest8<T>(b[i], largest8<T>(a[i], m));
+    } else {
+        for (int u = lane; u < total; u += 64) { const uint4 *p = source(u); m = largest8<T>(p[1], largest8<T>(p[0], m)); }
+    }
+    const Scale c = new_scale<T>(m, old, off);
+    auto put = [&](int u, const uint4 &lo, const uint4 &hi) {
+        const uint2 e = encode8<T>(lo, c.inv), f = encode8<T>(hi, c.inv);
+        *target(u) = make_uint4(e.x, e.y, f.x, f.y);
+    };
+    if (held) {
+#pragma unroll
+        for (int i = 0; i < K_HELD; ++i)
+            if (64 * i + lane < total) put(64 * i + lane, a[i], b[i]);
+    } else {
+        for (int u = lane; u < total; u += 64) { const uint4 *p = source(u); put(u, p[0], p[1]); }
+    }
+    if (c.raised)                                          // the older tokens lie in front
+        for (int u = -1 - lane; u >= -off * pieces; u -= 64) {
+            const uint4 v = *target(u);
+            *target(u) = make_uint4(recode4(v.x, c.factor), recode4(v.y, c.factor), recode4(v.z, c.factor), recode4(v.w, c.factor));
+        }
+    if (lane == 0) *scale = c.value;
+}
+
+// Values: item u = the sixteen tokens of a strip, two columns; strips from the first one with a new token on.
+template <typename T> __device__ __forceinline__ void store_values(const StoreParams &kp, int t0, int block, int off, int n, int s, int lane)
+{
+    const size_t unit = (size_t)block * kp.S + s;
+    const int first = off >> 4, pairs = kp.d_pool / 2, total = (((off + n - 1) >> 4) - first + 1) * pairs;
+    const uint16_t *x = (const uint16_t *)kp.POOL + (size_t)s * kp.d_pool;
+    uint8_t *dst = kp.pool_q8 + unit * kp.page * kp.d_pool;
+    float *scale = kp.scales + 2 * unit;
+    const bool held = total <= 64 * V_HELD;
+    struct Item { uint32_t w[16]; uint4 old[2]; };         // new values of the places that have one, what the two pieces hold
+    // places of strip `strip` that get a new token: [lo, hi)
+    auto places = [&](int strip, int &lo, int &hi) { lo = off - 16 * strip; hi = lo + n; };
+    auto target = [&](int strip, int pair) { return reinterpret_cast<uint4 *>(dst + ((size_t)strip * kp.d_pool + 2 * pair) * 16); };
+    auto load = [&](int u, Item &it) {
+        const int at = quotient(u, kp.pairs_magic), strip = first + at, pair = u - at * pairs;
+        int lo, hi;
+        places(strip, lo, hi);
+        const uint16_t *p = x + (size_t)(t0 - lo) * kp.pool_row + 2 * pair;          // of place 0 (read from the first new one on)
+        if (lo <= 0 && hi >= 16) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) it.w[i] = *reinterpret_cast<const uint32_t *>(p + (size_t)i * kp.pool_row);
+            it.old[0] = it.old[1] = make_uint4(0, 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) it.w[i] = i >= lo && i < hi ? *reinterpret_cast<const uint32_t *>(p + (ptrdiff_t)i * (ptrdiff_t)kp.pool_row) : 0;
+            it.old[0] = target(strip, pair)[0];
+            it.old[1] = target(strip, pair)[1];
+        }
+    };
+    auto largest = [&](const Item &it, float m) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float2 f = unpack2<T>(it.w[i]);
+            m = fmaxf(m, fmaxf(fabsf(f.x), fabsf(f.y)));
+        }
+        return m;
+    };
+    auto put = [&](int u, const Item &it, const Scale &c) {
+        const int at = quotient(u, kp.pairs_magic), strip = first + at, pair = u - at * pairs;
+        int lo, hi;
+        places(strip, lo, hi);
+        unsigned o[2][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float2 f[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f[j] = unpack2<T>(it.w[4 * i + j]);
+            o[0][i] = encode4(in_range(f[0].x, c.inv), in_range(f[1].x, c.inv), in_range(f[2].x, c.inv), in_range(f[3].x, c.inv));
+            o[1][i] = encode4(in_range(f[0].y, c.inv), in_range(f[1].y, c.inv), in_range(f[2].y, c.inv), in_range(f[3].y, c.inv));
+        }
+        if (lo > 0 || hi < 16) {                           // older tokens (recoded if the scale rose) and places behind the new ones stay
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int from = min(max(lo - 4 * i, 0), 4), to = min(max(hi - 4 * i, 0), 4);
+                const unsigned older = from == 4 ? 0xFFFFFFFFu : (1u << (8 * from)) - 1, upto = to == 4 ? 0xFFFFFFFFu : (1u << (8 * to)) - 1;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const unsigned h = i == 0 ? it.old[k].x : i == 1 ? it.old[k].y : i == 2 ? it.old[k].z : it.old[k].w;
+                    const unsigned front = c.raised ? recode4(h, c.factor) : h;
+                    o[k][i] = (front & older) | (o[k][i] & upto & ~older) | (h & ~(upto | older));
+                }
+            }
+        }
+        uint4 *p = target(strip, pair);
+        p[0] = make_uint4(o[0][0], o[0][1], o[0][2], o[0][3]);
+        p[1] = make_uint4(o[1][0], o[1][1], o[1][2], o[1][3]);
+    };
+    Item it[V_HELD];
+    float m = 0.f;
+    const float old = off > 0 ? *scale : 0.f;
+    if (held) {
+#pragma unroll
+        for (int i = 0; i < V_HELD; ++i)
+            if (64 * i + lane < total) load(64 * i + lane, it[i]);
+            else
+#pragma unroll
+                for (int j = 0; j < 16; ++j) it[i].w[j] = 0;
+#pragma unroll
+        for (int i = 0; i < V_HELD; ++i) m = largest(it[i], m);
+    } else {
+        for (int u = lane; u < total; u += 64) { load(u, it[0]); m = largest(it[0], m); }
+    }
+    const Scale c = new_scale<T>(m, old, off);
+    if (held) {
+#pragma unroll
+        for (int i = 0; i < V_HELD; ++i)
+            if (64 * i + lane < total) put(64 * i + lane, it[i], c);
+    } else {
+        for (int u = lane; u < total; u += 64) { load(u, it[0]); put(u, it[0], c); }
+    }
+    if (c.raised)                                          // strips of older tokens alone
+        for (int u = lane; u < first * kp.d_pool; u += 64) {
+            uint4 *p = reinterpret_cast<uint4 *>(dst) + u;
+            const uint4 v = *p;
+            *p = make_uint4(recode4(v.x, c.factor), recode4(v.y, c.factor), recode4(v.z, c.factor), recode4(v.w, c.factor));
+        }
+    if (lane == 0) *scale = c.value;
+}
+
+// A wavefront takes the units that start among `window` packed rows, one KV head, one component.  A unit starts where a token's slot
+// does not follow the slot of the token in front of it, or opens a block, and ends where either happens again.
 template <typename T>
 __global__ __launch_bounds__(256) void page_store_kernel(const StoreParams kp)
 {
-    __shared__ float maxima[2][4];
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int win = blockIdx.x / kp.S, s = blockIdx.x - win * kp.S;
+    const int lane = threadIdx.x & 63;
+    const long job = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int win = (int)(job / (2 * kp.S)), s = (int)(job - (long)win * 2 * kp.S) >> 1;
+    const bool keys = (job & 1) != 0;
     const int slots = kp.n_blocks * kp.page;
     const int lo = win * kp.window, hi = min(lo + kp.window, kp.T);          // at most 64 rows
     const int t = lo + lane;
     const int mine = t < hi ? kp.slot[t] : -1, before = t < hi && t > 0 ? kp.slot[t - 1] : -1;
     const bool valid = (unsigned)mine < (unsigned)slots;
     unsigned long long starts = __builtin_amdgcn_ballot_w64(valid && (mine % kp.page == 0 || before < 0 || mine != before + 1));
-    for (; starts != 0; starts &= starts - 1) {                              // (the same for every wavefront)
+    for (; starts != 0; starts &= starts - 1) {
         const int at = __builtin_ctzll(starts), first = __builtin_amdgcn_readlane(mine, at), t0 = lo + at;
         const int block = first / kp.page, off = first - block * kp.page;
         const int most = min(kp.page - off, kp.T - t0);                      // >= 1
@@ -204,7 +269,8 @@ __global__ __launch_bounds__(256) void page_store_kernel(const StoreParams kp)
             n += run;
             if (run < 64) break;
         }
-        store_unit<T>(kp, t0, block, off, n, s, maxima, tid);
+        if (keys) store_keys<T>(kp, t0, block, off, n, s, lane);
+        else store_values<T>(kp, t0, block, off, n, s, lane);
     }
 }
 
@@ -213,11 +279,13 @@ __global__ __launch_bounds__(256) void page_store_kernel(const StoreParams kp)
 hipError_t launch_page_store_q8(const StoreArgs &a, hipStream_t st)
 {
     const ServeDims &d = a.d;
-    // A workgroup per token where requests bring a few (each is a unit of its own), else one per block's worth of tokens: most
-    // of them start one unit, and a workgroup per token would be started for nothing page - 1 times of page.
+    auto magic = [](int n) { return n == 1 ? 0u : (unsigned)((1ull << 32) / (unsigned)n + 1); };
+    // Wavefronts per token where requests bring a few (each is a unit of its own), else per block's worth of tokens: most of them start
+    // one unit, and wavefronts per token would be started for nothing page - 1 times of page.
     const int window = d.max_q <= 8 ? 1 : d.page < 64 ? d.page : 64;
-    const StoreParams kp{a.SEL, a.POOL, a.slot, a.sel_q8, a.pool_q8, a.scales, d.T, d.S, d.d_pool, d.d_sel, d.page, d.n_blocks, window, d.sel_row, d.pool_row};
-    const unsigned grid = (unsigned)(((long)d.T + window - 1) / window * d.S);
+    const StoreParams kp{a.SEL, a.POOL, a.slot, a.sel_q8, a.pool_q8, a.scales, d.T, d.S, d.d_pool, d.d_sel, d.page, d.n_blocks, window,
+                         magic(d.d_sel / 16), magic(d.d_pool / 2), d.sel_row, d.pool_row};
+    const unsigned grid = (unsigned)((((long)d.T + window - 1) / window * d.S * 2 + 3) / 4);
     if (grid == 0) return hipSuccess;
     if (d.dtype == LCA_F16) page_store_kernel<f16_t><<<grid, 256, 0, st>>>(kp);
     else page_store_kernel<uint16_t><<<grid, 256, 0, st>>>(kp);

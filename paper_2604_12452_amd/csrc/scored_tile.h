@@ -24,6 +24,7 @@
 #pragma once
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "serve_row.h"
 
@@ -69,6 +70,10 @@ template <typename E> __device__ __forceinline__ uint4 convert8(unsigned lo, uns
 {
     return make_uint4(convert2<E>(lo, scale, false), convert2<E>(lo, scale, true), convert2<E>(hi, scale, false), convert2<E>(hi, scale, true));
 }
+
+// f(0), f(1), .. with the numbers as constants.
+template <int... I, typename F> __device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F &&f) { (f(std::integral_constant<int, I>()), ...); }
+template <int N, typename F> __device__ __forceinline__ void each(F &&f) { each_of(std::make_integer_sequence<int, N>(), f); }
 
 struct TileParams {
     const void *Q, *SEL, *POOL;
@@ -418,9 +423,10 @@ __global__ __launch_bounds__(64 * NW, DV <= 128 ? 2 : 1) void scored_tile_kernel
         if constexpr (PAGED) fast = fast && (valid & 0xF) == 0xF;
         return fast;
     };
-    // Slot of half HF of a tile that is: weights to the references as they are, one or two scores behind every MFMA, operands
-    // requested RING MFMAs ahead.  Returns the lane's sum.
-    constexpr int MFMAS = NKS + 2 * NDV, RING = 3;
+    // Slot of half HF of a tile that is: weights to the references as they are.  A score goes through its stages in as many steps
+    // (one MFMA each), so that nothing waits for the instruction in front of it: A its logit, with a cap the exponential in it,
+    // B the cap's reciprocal, C the weight, D sum and rounding.  Operands are requested RING MFMAs ahead.  Returns the lane's sum.
+    constexpr int MFMAS = NKS + 2 * NDV, RING = 3, LAST = CAP ? 3 : 2;
     auto fast_slot = [&](auto HF, int t) __attribute__((always_inline)) {
         constexpr int hf = decltype(HF)::value;
         constexpr std::integral_constant<int, hf ^ 1> OTHER;
@@ -430,28 +436,32 @@ __global__ __launch_bounds__(64 * NW, DV <= 128 ? 2 : 1) void scored_tile_kernel
         ex8 ring[RING];
 #pragma unroll
         for (int i = 0; i < RING; ++i) ring[i] = request(i);
-        float sum[2] = {0.f, 0.f}, even = 0.f;
+        float sum[2] = {0.f, 0.f}, x[16];
         const float top = (CAP ? kp.rule.cap_log2 : 0.f) - m_run, bias = BIAS ? fmaf(slope, (float)(first_key(t) + 32 * hf + 8 * h32 - pos), top) : top;
         LCA_FENCE();
-#pragma unroll
-        for (int i = 0; i < MFMAS; ++i) {
-            if (i < 2 * NDV) acc[i % NDV] = mfma_32x32x16(ring[i % RING], __builtin_bit_cast(ex8, pb[hf ^ 1][i / NDV]), acc[i % NDV]);
+        each<MFMAS>([&](auto I) __attribute__((always_inline)) {
+            constexpr int i = decltype(I)::value;
+            if constexpr (i < 2 * NDV) acc[i % NDV] = mfma_32x32x16(ring[i % RING], __builtin_bit_cast(ex8, pb[hf ^ 1][i / NDV]), acc[i % NDV]);
             else sv[hf ^ 1] = mfma_32x32x16(ring[i % RING], qf[i - 2 * NDV], i == 2 * NDV ? floatx16{} : sv[hf ^ 1]);
-            if (i + RING < MFMAS) ring[i % RING] = request(i + RING);
-#pragma unroll
-            for (int c = i * 16 / MFMAS; c < (i + 1) * 16 / MFMAS; ++c) {
+            if constexpr (i + RING < MFMAS) ring[i % RING] = request(i + RING);
+            each<16>([&](auto C) __attribute__((always_inline)) {
+                constexpr int c = decltype(C)::value, at = i - c * (MFMAS - LAST) / 16;        // steps since this score's first
                 const float off = BIAS ? fmaf(slope, (float)((c & 7) + 16 * (c >> 3)), bias) : bias;
-                float x;
-                if constexpr (CAP) x = fmaf(-2.f * kp.rule.cap_log2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(sv[hf][c] * kp.rule.pre)), off);
-                else x = fmaf(sv[hf][c], kp.rule.scale_log2, off);
-                float p = __builtin_amdgcn_exp2f(x);
-                asm volatile("" : "+v"(p));                                    // here, and not where it is used
-                sum[c & 1] += p;
-                if (c & 1) pb[hf][c >> 3][(c & 7) >> 1] = pack(even, p);
-                else even = p;
-            }
+                if constexpr (at == LAST) {
+                    sum[c & 1] += x[c];
+                    if constexpr (c & 1) {
+                        unsigned w = pack(x[c - 1], x[c]);
+                        asm volatile("" : "+v"(w));                            // (here, and not where it is used)
+                        pb[hf][c >> 3][(c & 7) >> 1] = w;
+                    }
+                }
+                if constexpr (at == LAST - 1) x[c] = __builtin_amdgcn_exp2f(CAP ? fmaf(-2.f * kp.rule.cap_log2, x[c], off) : x[c]);
+                if constexpr (CAP && at == 1) x[c] = __builtin_amdgcn_rcpf(1.f + x[c]);
+                if constexpr (at == 0) x[c] = CAP ? __builtin_amdgcn_exp2f(sv[hf][c] * kp.rule.pre) : fmaf(sv[hf][c], kp.rule.scale_log2, off);
+            });
             LCA_FENCE();
-        }
+        });
+        asm volatile("" : "+v"(sum[0]), "+v"(sum[1]));
         return sum[0] + sum[1];
     };
     auto slow_weights = [&](auto HF, int t) __attribute__((always_inline)) {
