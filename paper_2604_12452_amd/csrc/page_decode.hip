@@ -63,6 +63,7 @@ struct DecodeParams {
     ScoreRule rule;
     int parts, per_part;                  // workgroups of a (request, KV head, group of columns); least tiles of one
     int groups;                           // groups of 16 NCT columns
+    FastDiv by_parts, by_groups;
     int most;                             // requests of more columns are left to the chunk kernel (INT_MAX: none)
 };
 
@@ -82,35 +83,38 @@ __device__ __forceinline__ Tiles make_tiles(const Request &r, int window)
     return t;
 }
 
-// A column's merged output: lanes hold V values each (columns lane * V ..) and the softmax's sum and maximum (base 2).  One that is not
-// finite is computed again over what its row sees alone (serve_row.h).
-template <typename E, int DV>
-__device__ __forceinline__ void finish_column(const DecodeParams &kp, const Request &r, int b, int s, int column, const float (&sum)[DV / 64], float l, float m, int lane)
+// A column computed again over what its row sees alone (serve_row.h).
+template <typename E, int DV> __device__ __forceinline__ void row_again(const DecodeParams &kp, const Request &r, int b, int s, int column, int lane)
 {
     typedef typename Store<E>::type T;
-    constexpr int V = DV / 64;
     const ServeDims &d = kp.d;
-    const int row = column / d.hps, h = s * d.hps + (column - row * d.hps), t = r.first + row;
-    T *O = (T *)kp.O + ((size_t)t * d.H + h) * d.d_pool;
-    float *lse = kp.lse != nullptr ? kp.lse + (size_t)t * d.H + h : nullptr;
-    bool fine = true;
+    const int row = d.by_hps(column), h = s * d.hps + (column - row * d.hps), t = r.first + row;
+    const PagedSource<T> src{kp.block_table + (size_t)b * d.max_blocks, kp.sel_q8, kp.pool_q8, kp.scales, d.page, d.n_blocks, d.S, s, d.d_sel, d.d_pool, d.by_page};
+    scored_row<T, DV / 64>(src, (const T *)kp.q + (size_t)t * d.q_row + (size_t)h * d.d_sel, r, r.pos0 + row, kp.slopes != nullptr ? kp.slopes[h] * LOG2E : 0.f, kp.rule, d.d_sel,
+                           d.d_pool, (T *)kp.O + ((size_t)t * d.H + h) * d.d_pool, kp.lse != nullptr ? kp.lse + (size_t)t * d.H + h : nullptr, lane);
+}
+
+// Output columns [first, first + N) of a column from its sums, the softmax's sum and maximum (base 2); whether they are finite numbers.
+template <typename E, int N>
+__device__ __forceinline__ bool write_column(const DecodeParams &kp, const Request &r, int s, int column, int first, const float (&sum)[N], float l, float m)
+{
+    typedef typename Store<E>::type T;
+    const ServeDims &d = kp.d;
+    const int row = d.by_hps(column), h = s * d.hps + (column - row * d.hps);
+    const size_t at = (size_t)(r.first + row) * d.H + h;
+    T *O = (T *)kp.O + at * d.d_pool + first;
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    float o[V];
+    bool fine = true;
+    T o[N];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        o[v] = sum[v] * inv;
-        fine = fine && fabsf(o[v]) < INFINITY;
+    for (int v = 0; v < N; ++v) {
+        const float x = sum[v] * inv;
+        fine = fine && fabsf(x) < INFINITY;
+        o[v] = from_float<T>(x);
     }
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!fine) != 0, 0)) {
-        const PagedSource<T> src{kp.block_table + (size_t)b * d.max_blocks, kp.sel_q8, kp.pool_q8, kp.scales, d.page, d.n_blocks, d.S, s, d.d_sel, d.d_pool};
-        scored_row<T, V>(src, (const T *)kp.q + (size_t)t * d.q_row + (size_t)h * d.d_sel, r, r.pos0 + row, kp.slopes != nullptr ? kp.slopes[h] * LOG2E : 0.f, kp.rule,
-                         d.d_sel, d.d_pool, O, lse, lane);
-        return;
-    }
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-        if (lane * V + v < d.d_pool) O[lane * V + v] = from_float<T>(o[v]);
-    if (lse != nullptr && lane == 0) *lse = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    if (first < d.d_pool) __builtin_memcpy(__builtin_assume_aligned(O, N * sizeof(T)), o, N * sizeof(T));        // (N divides 16, and 16 the width)
+    if (kp.lse != nullptr && first == 0) kp.lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    return fine;
 }
 
 template <typename E, int DK, int DV, int NCT>
@@ -124,9 +128,9 @@ __global__ __launch_bounds__(256, 2) void page_decode_kernel(const DecodeParams 
     const ServeDims &d = kp.d;
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, q4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int unit = blockIdx.x / kp.parts, part = blockIdx.x - unit * kp.parts;
-    const int pair = unit / kp.groups, group = unit - pair * kp.groups;
-    const int b = pair / d.S, s = pair - b * d.S;
+    const int unit = kp.by_parts((int)blockIdx.x), part = blockIdx.x - unit * kp.parts;
+    const int pair = kp.by_groups(unit), group = unit - pair * kp.groups;
+    const int b = d.by_S(pair), s = pair - b * d.S;
     const Request r = make_request(kp.q_start, kp.seq_len, kp.prefix_len, b, d.T, d.max_blocks * d.page);
     const int columns = r.rows * d.hps;
     if (columns == 0 || columns > kp.most) return;
@@ -135,7 +139,7 @@ __global__ __launch_bounds__(256, 2) void page_decode_kernel(const DecodeParams 
     const bool many = columns > kp.groups * 16 * NCT;
     const int parts = many ? 1 : kp.parts;
     if (part >= parts) return;
-    const int per = max(kp.per_part, (tiles.count + parts - 1) / parts);
+    const int per = max(kp.per_part, many ? tiles.count : kp.by_parts(tiles.count + kp.parts - 1));
     const int lo = part * per, hi = many ? tiles.count : min(lo + per, tiles.count);
     if (lo >= hi && part > 0) return;                                          // (nothing to see at all: part 0 writes it)
     const bool whole = lo == 0 && hi == tiles.count;                           // this workgroup has the request to itself
@@ -152,7 +156,7 @@ __global__ __launch_bounds__(256, 2) void page_decode_kernel(const DecodeParams 
         ex8 qf[NCT][2 * NK];
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct) {
-            const int c = min(c0 + 16 * ct + col, columns - 1), row = c / d.hps, h = s * d.hps + (c - row * d.hps);
+            const int c = min(c0 + 16 * ct + col, columns - 1), row = d.by_hps(c), h = s * d.hps + (c - row * d.hps);
             pos[ct] = r.pos0 + row;
             slope[ct] = kp.slopes != nullptr ? kp.slopes[h] * LOG2E : 0.f;
             const E *qp = (const E *)kp.q + (size_t)(r.first + row) * d.q_row + (size_t)h * d.d_sel;
@@ -175,7 +179,7 @@ __global__ __launch_bounds__(256, 2) void page_decode_kernel(const DecodeParams 
         auto tile_at = [&](int x) { return x < tiles.pre ? x : x - tiles.pre + tiles.from; };
         // the blocks of a lane's two strips of tile x: the one its key rows lie in, the one of its values; -1: none
         auto block_of = [&](int strip) {
-            const int blk = table[min(strip, strip_end - 1) / strips];
+            const int blk = table[d.by_strips(min(strip, strip_end - 1))];
             return strip < strip_end && (unsigned)blk < (unsigned)d.n_blocks ? blk : -1;
         };
         uint4 kreg[4][NK], vreg[NV];
@@ -192,7 +196,7 @@ __global__ __launch_bounds__(256, 2) void page_decode_kernel(const DecodeParams 
             const int strip = 4 * tile_at(x) + (col >> 2);
             k_blk = k_next;
             const size_t u = (size_t)max(k_blk, 0) * d.S + s;
-            const uint8_t *p = kp.sel_q8 + (u * d.page + (strip % strips) * 16 + (col & 3)) * d.d_sel + 16 * q4;
+            const uint8_t *p = kp.sel_q8 + (u * d.page + (strip - d.by_strips(strip) * strips) * 16 + (col & 3)) * d.d_sel + 16 * q4;
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -204,7 +208,7 @@ __global__ __launch_bounds__(256, 2) void page_decode_kernel(const DecodeParams 
             const int strip = 4 * tile_at(x) + q4;
             v_blk = v_next;
             const size_t u = (size_t)max(v_blk, 0) * d.S + s;
-            const uint8_t *p = kp.pool_q8 + ((u * strips + strip % strips) * d.d_pool + col) * 16;
+            const uint8_t *p = kp.pool_q8 + ((u * strips + strip - d.by_strips(strip) * strips) * d.d_pool + col) * 16;
 #pragma unroll
             for (int v = 0; v < NV; ++v)
                 if (v < cols16) vreg[v] = *reinterpret_cast<const uint4 *>(p + 256 * v);
@@ -338,28 +342,41 @@ __global__ __launch_bounds__(256, 2) void page_decode_kernel(const DecodeParams 
             l_ct = lanes::across32(lanes::across16(l_ct, lanes::Sum()), lanes::Sum());
             if (q4 == 0) { stats[wave][col][0] = m_ct; stats[wave][col][1] = l_ct; }
             __syncthreads();
-            for (int k = wave; k < 16 && c0 + 16 * ct + k < columns; k += 4) {
-                float m = -INFINITY, l = 0.f, sum[DV / 64], f[4];
+            {
+                // sixteen lanes take a column, DV / 16 outputs each
+                constexpr int N = DV / 16;
+                const int k = wave * 4 + q4, column = c0 + 16 * ct + k, first = col * N;
+                float m = -INFINITY, l = 0.f, sum[N], f[4];
 #pragma unroll
                 for (int w = 0; w < 4; ++w) m = fmaxf(m, stats[w][k][0]);
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     f[w] = stats[w][k][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stats[w][k][0] - m);
-                    l += stats[w][k][1] * f[w];
+                    l = fmaf(stats[w][k][1], f[w], l);
                 }
 #pragma unroll
-                for (int v = 0; v < DV / 64; ++v) {
-                    sum[v] = 0.f;
+                for (int v = 0; v < N; ++v) sum[v] = 0.f;
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) sum[v] = fmaf(outs[w][k][lane * (DV / 64) + v], f[w], sum[v]);
-                }
+                for (int w = 0; w < 4; ++w)
+#pragma unroll
+                    for (int v = 0; v < N; v += 4) {
+                        const floatx4 y = *reinterpret_cast<const floatx4 *>(&outs[w][k][first + v]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sum[v + i] = fmaf(y[i], f[w], sum[v + i]);
+                    }
                 if (whole) {
-                    finish_column<E, DV>(kp, r, b, s, c0 + 16 * ct + k, sum, l, m, lane);
+                    const bool fine = column >= columns || write_column<E, N>(kp, r, s, column, first, sum, l, m);
+                    unsigned long long odd = __builtin_amdgcn_ballot_w64(!fine);
+                    while (__builtin_expect(odd != 0, 0)) {
+                        const int g = __builtin_ctzll(odd) >> 4;
+                        row_again<E, DV>(kp, r, b, s, c0 + 16 * ct + wave * 4 + g, lane);
+                        odd &= ~(0xFFFFull << (16 * g));
+                    }
                 } else {
                     float *dst = kp.part + (((size_t)unit * kp.parts + part) * 16 * NCT + 16 * ct + k) * (DV + 2);
 #pragma unroll
-                    for (int v = 0; v < DV / 64; ++v) dst[2 + lane * (DV / 64) + v] = sum[v];
-                    if (lane == 0) { dst[0] = m; dst[1] = l; }
+                    for (int v = 0; v < N; v += 2) *reinterpret_cast<float2 *>(dst + 2 + first + v) = float2{sum[v], sum[v + 1]};
+                    if (col == 0) *reinterpret_cast<float2 *>(dst) = float2{m, l};
                 }
             }
             __syncthreads();
@@ -368,39 +385,28 @@ __global__ __launch_bounds__(256, 2) void page_decode_kernel(const DecodeParams 
 }
 
 // Joins the parts of every column that has more than one: one wavefront per column.
-template <typename E, int DV>
-__global__ __launch_bounds__(256) void page_merge_kernel(const DecodeParams kp, int columns_per_unit)
+template <typename E, int DV, int NCT>
+__global__ __launch_bounds__(256) void page_merge_kernel(const DecodeParams kp)
 {
-    constexpr int V = DV / 64;
+    constexpr int V = DV / 64, columns_per_unit = 16 * NCT;
     const ServeDims &d = kp.d;
     const int lane = threadIdx.x & 63;
-    const long c = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int unit = (int)(c / columns_per_unit), k = (int)(c - (long)unit * columns_per_unit);
-    const int pair = unit / kp.groups, group = unit - pair * kp.groups, b = pair / d.S, s = pair - b * d.S;
+    const int c = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int unit = c / columns_per_unit, k = c % columns_per_unit;         // (a power of two)
+    const int pair = kp.by_groups(unit), group = unit - pair * kp.groups, b = d.by_S(pair), s = pair - b * d.S;
     if (b >= d.B) return;
     const Request r = make_request(kp.q_start, kp.seq_len, kp.prefix_len, b, d.T, d.max_blocks * d.page);
     const int columns = r.rows * d.hps, column = group * columns_per_unit + k;
     if (column >= columns || columns > kp.most || columns > kp.groups * columns_per_unit) return;
     const Tiles tiles = make_tiles(r, kp.rule.window);
-    const int per = max(kp.per_part, (tiles.count + kp.parts - 1) / kp.parts);
+    const int per = max(kp.per_part, kp.by_parts(tiles.count + kp.parts - 1));
     if (tiles.count <= per) return;                                            // one part: it has written the output
     const int parts = (tiles.count + per - 1) / per;
     const float *src = kp.part + ((size_t)unit * kp.parts * columns_per_unit + k) * (DV + 2);
-    const size_t step = (size_t)columns_per_unit * (DV + 2);
-    float m = -INFINITY, l = 0.f, sum[V];
-    for (int p = lane; p < parts; p += 64) m = fmaxf(m, src[p * step]);
-    m = lanes::over_group<64>(m, lanes::Max());
-#pragma unroll
-    for (int v = 0; v < V; ++v) sum[v] = 0.f;
-#pragma unroll 4
-    for (int p = 0; p < parts; ++p) {
-        const float *x = src + p * step;
-        const float f = x[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[0] - m);
-        l = fmaf(x[1], f, l);
-#pragma unroll
-        for (int v = 0; v < V; ++v) sum[v] = fmaf(x[2 + lane * V + v], f, sum[v]);
-    }
-    finish_column<E, DV>(kp, r, b, s, column, sum, l, m, lane);
+    float m, l, sum[V];
+    merge_parts<V>(src, (size_t)columns_per_unit * (DV + 2), parts, lane, m, l, sum);
+    const bool fine = write_column<E, V>(kp, r, s, column, lane * V, sum, l, m);
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!fine) != 0, 0)) row_again<E, DV>(kp, r, b, s, column, lane);
 }
 
 struct Plan { int nct, groups, parts, per_part; };
@@ -425,28 +431,28 @@ Plan make_plan(const ServeDims &d)
     return p;
 }
 
-template <typename E, int DK, int DV> void run(const DecodeParams &kp, const Plan &p, hipStream_t st)
+template <typename E, int DK, int DV, int NCT> void run(const DecodeParams &kp, hipStream_t st)
 {
-    const ServeDims &d = kp.d;
-    const unsigned grid = (unsigned)((long)d.B * d.S * p.groups * p.parts);
+    const long units = (long)kp.d.B * kp.d.S * kp.groups;
+    page_decode_kernel<E, DK, DV, NCT><<<(unsigned)(units * kp.parts), 256, 0, st>>>(kp);
+    if (kp.parts > 1) page_merge_kernel<E, DV, NCT><<<(unsigned)(units * 4 * NCT), 256, 0, st>>>(kp);
+}
+template <typename E, int DK, int DV> void run_columns(const DecodeParams &kp, const Plan &p, hipStream_t st)
+{
     if constexpr (DV == 64)
-        if (p.nct == 4) page_decode_kernel<E, DK, DV, 4><<<grid, 256, 0, st>>>(kp);
+        if (p.nct == 4) return run<E, DK, DV, 4>(kp, st);
     if constexpr (DV <= 128)
-        if (p.nct == 2) page_decode_kernel<E, DK, DV, 2><<<grid, 256, 0, st>>>(kp);
-    if (p.nct == 1) page_decode_kernel<E, DK, DV, 1><<<grid, 256, 0, st>>>(kp);
-    if (p.parts > 1) {
-        const long columns = (long)d.B * d.S * p.groups * 16 * p.nct;
-        page_merge_kernel<E, DV><<<(unsigned)((columns + 3) / 4), 256, 0, st>>>(kp, 16 * p.nct);
-    }
+        if (p.nct == 2) return run<E, DK, DV, 2>(kp, st);
+    run<E, DK, DV, 1>(kp, st);
 }
 
 template <typename E> void run_widths(const DecodeParams &kp, const Plan &p, hipStream_t st)
 {
     const int dk = kp.d.d_sel, dv = kp.d.d_pool;
-    if (dk <= 64 && dv <= 64) run<E, 64, 64>(kp, p, st);
-    else if (dk <= 128 && dv <= 128) run<E, 128, 128>(kp, p, st);
-    else if (dk <= 192 && dv <= 128) run<E, 192, 128>(kp, p, st);
-    else run<E, 256, 256>(kp, p, st);
+    if (dk <= 64 && dv <= 64) run_columns<E, 64, 64>(kp, p, st);
+    else if (dk <= 128 && dv <= 128) run_columns<E, 128, 128>(kp, p, st);
+    else if (dk <= 192 && dv <= 128) run_columns<E, 192, 128>(kp, p, st);
+    else run_columns<E, 256, 256>(kp, p, st);
 }
 
 }  // namespace
@@ -462,7 +468,7 @@ hipError_t launch_page_decode(const ScoredArgs &a, int most, hipStream_t st)
 {
     const Plan p = make_plan(a.d);
     const DecodeParams kp{a.Q, a.O, a.lse, a.part, a.q_start, a.seq_len, a.prefix_len, a.block_table, a.slopes, a.sel_q8, a.pool_q8, a.scales, a.d, score_rule(a.d),
-                          p.parts, p.per_part, p.groups, most};
+                          p.parts, p.per_part, p.groups, FastDiv(p.parts), FastDiv(p.groups), most};
     if (a.d.dtype == LCA_F16) run_widths<_Float16>(kp, p, st);
     else run_widths<__bf16>(kp, p, st);
     return hipGetLastError();

@@ -21,12 +21,9 @@ struct StoreParams {
     uint8_t *sel_q8, *pool_q8;
     float *scales;
     int T, S, d_pool, d_sel, page, n_blocks, window;       // window: packed rows a wavefront looks for starts of units in
-    unsigned pieces_magic, pairs_magic;                    // for divisions by d_sel / 16 and d_pool / 2 (quotient)
+    FastDiv by_pieces, by_pairs, by_S2, by_page;           // d_sel / 16, d_pool / 2, 2 S
     size_t sel_row, pool_row;
 };
-
-// x / d for x * d < 2^32, with magic = 2^32 / d + 1 (rounded down; d >= 2), or 0 for d = 1.
-__device__ __forceinline__ int quotient(int x, unsigned magic) { return magic == 0 ? x : (int)__umulhi((unsigned)x, magic); }
 
 template <typename T> struct Range;                      // exponents of a block's scale: the decoded codes stay finite numbers of the type
 template <> struct Range<uint16_t> { static constexpr int LO = -100, HI = 119; };
@@ -105,7 +102,7 @@ template <typename T> __device__ __forceinline__ void store_keys(const StorePara
     const int pieces = kp.d_sel / 16, total = n * pieces;
     const bool held = total <= 64 * K_HELD;
     auto source = [&](int u) {
-        const int t = quotient(u, kp.pieces_magic);
+        const int t = kp.by_pieces(u);
         return reinterpret_cast<const uint4 *>(x + (size_t)t * kp.sel_row + 16 * (u - t * pieces));
     };
     auto target = [&](int u) { return reinterpret_cast<uint4 *>(dst + 16 * (size_t)u); };      // (tokens of a block follow one another)
@@ -157,7 +154,7 @@ template <typename T> __device__ __forceinline__ void store_values(const StorePa
     auto places = [&](int strip, int &lo, int &hi) { lo = off - 16 * strip; hi = lo + n; };
     auto target = [&](int strip, int pair) { return reinterpret_cast<uint4 *>(dst + ((size_t)strip * kp.d_pool + 2 * pair) * 16); };
     auto load = [&](int u, Item &it) {
-        const int at = quotient(u, kp.pairs_magic), strip = first + at, pair = u - at * pairs;
+        const int at = kp.by_pairs(u), strip = first + at, pair = u - at * pairs;
         int lo, hi;
         places(strip, lo, hi);
         const uint16_t *p = x + (size_t)(t0 - lo) * kp.pool_row + 2 * pair;          // of place 0 (read from the first new one on)
@@ -181,7 +178,7 @@ template <typename T> __device__ __forceinline__ void store_values(const StorePa
         return m;
     };
     auto put = [&](int u, const Item &it, const Scale &c) {
-        const int at = quotient(u, kp.pairs_magic), strip = first + at, pair = u - at * pairs;
+        const int at = kp.by_pairs(u), strip = first + at, pair = u - at * pairs;
         int lo, hi;
         places(strip, lo, hi);
         unsigned o[2][4];
@@ -248,18 +245,18 @@ template <typename T>
 __global__ __launch_bounds__(256) void page_store_kernel(const StoreParams kp)
 {
     const int lane = threadIdx.x & 63;
-    const long job = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int win = (int)(job / (2 * kp.S)), s = (int)(job - (long)win * 2 * kp.S) >> 1;
+    const int job = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);     // (T * S < 2^30)
+    const int win = kp.by_S2(job), s = (job - win * 2 * kp.S) >> 1;
     const bool keys = (job & 1) != 0;
     const int slots = kp.n_blocks * kp.page;
     const int lo = win * kp.window, hi = min(lo + kp.window, kp.T);          // at most 64 rows
     const int t = lo + lane;
     const int mine = t < hi ? kp.slot[t] : -1, before = t < hi && t > 0 ? kp.slot[t - 1] : -1;
     const bool valid = (unsigned)mine < (unsigned)slots;
-    unsigned long long starts = __builtin_amdgcn_ballot_w64(valid && (mine % kp.page == 0 || before < 0 || mine != before + 1));
+    unsigned long long starts = __builtin_amdgcn_ballot_w64(valid && (mine == kp.by_page(mine) * kp.page || before < 0 || mine != before + 1));
     for (; starts != 0; starts &= starts - 1) {
         const int at = __builtin_ctzll(starts), first = __builtin_amdgcn_readlane(mine, at), t0 = lo + at;
-        const int block = first / kp.page, off = first - block * kp.page;
+        const int block = kp.by_page(first), off = first - block * kp.page;
         const int most = min(kp.page - off, kp.T - t0);                      // >= 1
         int n = 0;
         for (;;) {                                                           // tokens of the unit, 64 at a time
@@ -279,12 +276,11 @@ __global__ __launch_bounds__(256) void page_store_kernel(const StoreParams kp)
 hipError_t launch_page_store_q8(const StoreArgs &a, hipStream_t st)
 {
     const ServeDims &d = a.d;
-    auto magic = [](int n) { return n == 1 ? 0u : (unsigned)((1ull << 32) / (unsigned)n + 1); };
     // Wavefronts per token where requests bring a few (each is a unit of its own), else per block's worth of tokens: most of them start
     // one unit, and wavefronts per token would be started for nothing page - 1 times of page.
     const int window = d.max_q <= 8 ? 1 : d.page < 64 ? d.page : 64;
     const StoreParams kp{a.SEL, a.POOL, a.slot, a.sel_q8, a.pool_q8, a.scales, d.T, d.S, d.d_pool, d.d_sel, d.page, d.n_blocks, window,
-                         magic(d.d_sel / 16), magic(d.d_pool / 2), d.sel_row, d.pool_row};
+                         FastDiv(d.d_sel / 16), FastDiv(d.d_pool / 2), FastDiv(2 * d.S), d.by_page, d.sel_row, d.pool_row};
     const unsigned grid = (unsigned)((((long)d.T + window - 1) / window * d.S * 2 + 3) / 4);
     if (grid == 0) return hipSuccess;
     if (d.dtype == LCA_F16) page_store_kernel<f16_t><<<grid, 256, 0, st>>>(kp);

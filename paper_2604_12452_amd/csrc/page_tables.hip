@@ -16,6 +16,7 @@ struct TablesParams {
     const int32_t *cached_len, *new_len, *free_list, *free_count;
     int32_t *free_left, *block_table, *q_start, *seq_len, *slot, *position, *request, *base;
     int B, T, page, n_blocks, max_blocks;
+    FastDiv by_page;
 };
 
 constexpr int REFUSED = -1;                       // base of a request that gets nothing
@@ -48,7 +49,7 @@ __device__ __forceinline__ void write_token(const TablesParams &kp, int t, int b
         const int cached = max(kp.cached_len[b], 0), base = kp.base[b];
         position = (int)((unsigned)cached + (unsigned)(t - first));
         if (base != REFUSED) {
-            const int col = position / kp.page, have = (cached + kp.page - 1) / kp.page;
+            const int col = kp.by_page(position), have = kp.by_page(cached + kp.page - 1);
             int32_t *entry = kp.block_table + (size_t)b * kp.max_blocks + col;
             int block;
             if (col >= have) {                    // (0 <= base - (col - have): the stack held the request's blocks)
@@ -81,8 +82,8 @@ __global__ __launch_bounds__(WAVES * 64) void tables_requests_kernel(const Table
         const int end = min(scan_up_to<WAVES>(add, T1, lds, tid) + rows, T1);
         const long total = (long)cached + add;
         const bool fits = real && cached >= 0 && asked >= 0 && end <= kp.T && total <= (long)kp.max_blocks * kp.page;
-        const int have = fits ? (cached + kp.page - 1) / kp.page : 0;
-        const int need = fits ? min(((int)total + kp.page - 1) / kp.page - have, P1) : 0;
+        const int have = fits ? kp.by_page(cached + kp.page - 1) : 0;
+        const int need = fits ? min(kp.by_page((int)total + kp.page - 1) - have, P1) : 0;
         const int upto = min(scan_up_to<WAVES>(need, P1, lds, tid) + blocks, P1);
         const bool ok = fits && (need == 0 || upto <= free);
         if (real) {
@@ -178,7 +179,7 @@ hipError_t launch_page_tables(const TablesArgs &a, hipStream_t st)
 {
     const ServeDims &d = a.d;
     const TablesParams kp{a.cached_len, a.new_len, a.free_list, a.free_count, a.free_left, a.block_table, a.q_start, a.seq_len, a.slot, a.position, a.request,
-                          a.base, d.B, d.T, d.page, d.n_blocks, d.max_blocks};
+                          a.base, d.B, d.T, d.page, d.n_blocks, d.max_blocks, d.by_page};
     if (d.T <= 4096) {
         if (d.B <= 64 && d.T <= 256) tables_requests_kernel<1, true><<<1, 64, 0, st>>>(kp);
         else tables_requests_kernel<16, true><<<1, 1024, 0, st>>>(kp);

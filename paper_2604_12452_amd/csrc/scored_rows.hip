@@ -34,7 +34,7 @@ __global__ __launch_bounds__(256) void scored_rows_kernel(const RowsParams kp)
     T *O = (T *)kp.O + ((size_t)t * d.H + h) * d.d_pool;
     float *lse = kp.lse != nullptr ? kp.lse + (size_t)t * d.H + h : nullptr;
     if constexpr (PAGED) {
-        const PagedSource<T> src{kp.block_table + (size_t)b * d.max_blocks, kp.sel_q8, kp.pool_q8, kp.scales, d.page, d.n_blocks, d.S, s, d.d_sel, d.d_pool};
+        const PagedSource<T> src{kp.block_table + (size_t)b * d.max_blocks, kp.sel_q8, kp.pool_q8, kp.scales, d.page, d.n_blocks, d.S, s, d.d_sel, d.d_pool, d.by_page};
         scored_row<T, NV>(src, q, r, i, slope, kp.rule, d.d_sel, d.d_pool, O, lse, lane);
     } else {
         const PackedSource<T> src{(const T *)kp.SEL + (size_t)r.first * d.sel_row + (size_t)s * d.d_sel,

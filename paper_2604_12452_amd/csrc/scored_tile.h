@@ -88,6 +88,7 @@ struct TileParams {
     int items;                                    // per KV head
     int least;                                    // requests of fewer (row, head) pairs per KV head are another kernel's
     int parts, per_part;                          // workgroups of an item; least tiles of one
+    FastDiv by_parts;
     float *part;                                  // their results, [item, KV head, part, BM, DV + 2]
 };
 
@@ -140,7 +141,7 @@ __device__ __forceinline__ int request_of_item(const int32_t *q_start, const Ser
 struct Tiles { int pre, from, count; };
 __device__ __forceinline__ Tiles make_tiles(const ServeDims &d, const ScoreRule &rule, const Request &r, int c_first, int columns)
 {
-    const int lo = max(r.pos0 + c_first / d.hps, 0), hi = r.pos0 + min(c_first + BM - 1, columns - 1) / d.hps;      // positions of its rows
+    const int lo = max(r.pos0 + d.by_hps(c_first), 0), hi = r.pos0 + d.by_hps(min(c_first + BM - 1, columns - 1));      // positions of its rows
     Tiles t;
     t.pre = hi >= 0 ? (r.prefix + BN - 1) / BN : 0;
     t.from = max(t.pre, (lo >= rule.window ? lo - rule.window + 1 : 0) / BN);
@@ -154,13 +155,13 @@ __device__ __forceinline__ void row_again(const TileParams &kp, const Request &r
 {
     typedef typename Store<E>::type T;
     const ServeDims &d = kp.d;
-    const int row = c / d.hps, head = s * d.hps + (c - row * d.hps), t = r.first + row;
+    const int row = d.by_hps(c), head = s * d.hps + (c - row * d.hps), t = r.first + row;
     const T *q = (const T *)kp.Q + (size_t)t * d.q_row + (size_t)head * d.d_sel;
     T *O = (T *)kp.O + ((size_t)t * d.H + head) * d.d_pool;
     float *lse = kp.lse != nullptr ? kp.lse + (size_t)t * d.H + head : nullptr;
     const float slope = kp.slopes != nullptr ? kp.slopes[head] * LOG2E : 0.f;
     if constexpr (PAGED) {
-        const PagedSource<T> src{kp.block_table + (size_t)b * d.max_blocks, kp.sel_q8, kp.pool_q8, kp.scales, d.page, d.n_blocks, d.S, s, d.d_sel, d.d_pool};
+        const PagedSource<T> src{kp.block_table + (size_t)b * d.max_blocks, kp.sel_q8, kp.pool_q8, kp.scales, d.page, d.n_blocks, d.S, s, d.d_sel, d.d_pool, d.by_page};
         scored_row<T, DV / 64>(src, q, r, r.pos0 + row, slope, kp.rule, d.d_sel, d.d_pool, O, lse, lane);
     } else {
         const PackedSource<T> src{(const T *)kp.SEL + (size_t)r.first * d.sel_row + (size_t)s * d.d_sel, (const T *)kp.POOL + (size_t)r.first * d.pool_row + (size_t)s * d.d_pool,
@@ -189,7 +190,7 @@ __global__ __launch_bounds__(64 * NW, DV <= 128 ? 2 : 1) void scored_tile_kernel
     const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, h32 = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     // one KV head's items follow one another at a distance of S (an XCD sees few heads), the last rows first
-    const int u = blockIdx.x / kp.parts, part = blockIdx.x - u * kp.parts, x = kp.items - 1 - u / d.S, s = u % d.S;
+    const int u = kp.by_parts((int)blockIdx.x), part = blockIdx.x - u * kp.parts, y = d.by_S(u), x = kp.items - 1 - y, s = u - y * d.S;
     int item0;
     const int b = request_of_item(kp.q_start, d, x, lane, item0);
     const Request r = make_request(kp.q_start, kp.seq_len, kp.prefix_len, b, d.T, d.max_blocks * d.page);
@@ -197,14 +198,14 @@ __global__ __launch_bounds__(64 * NW, DV <= 128 ? 2 : 1) void scored_tile_kernel
     if (x < item0 || c_first >= columns || columns < kp.least) return;
 
     // this lane's column
-    const int c_lane = c_first + 32 * wave + n32, c = min(c_lane, columns - 1), row = c / d.hps, head = s * d.hps + (c - row * d.hps);
+    const int c_lane = c_first + 32 * wave + n32, c = min(c_lane, columns - 1), row = d.by_hps(c), head = s * d.hps + (c - row * d.hps);
     const int pos = r.pos0 + row, pre_lane = pos >= 0 ? r.prefix : 0, lo_lane = pos >= kp.rule.window ? pos - kp.rule.window + 1 : 0;
     const float slope = kp.slopes != nullptr ? kp.slopes[head] * LOG2E : 0.f;
     // positions of the wavefront's and of the item's rows
-    const int w_lo = __builtin_amdgcn_readfirstlane(r.pos0 + min(c_first + 32 * wave, columns - 1) / d.hps);
-    const int w_hi = __builtin_amdgcn_readfirstlane(r.pos0 + min(c_first + 32 * wave + 31, columns - 1) / d.hps);
+    const int w_lo = __builtin_amdgcn_readfirstlane(r.pos0 + d.by_hps(min(c_first + 32 * wave, columns - 1)));
+    const int w_hi = __builtin_amdgcn_readfirstlane(r.pos0 + d.by_hps(min(c_first + 32 * wave + 31, columns - 1)));
     const Tiles tiles = make_tiles(d, kp.rule, r, c_first, columns);
-    const int per = max(kp.per_part, (tiles.count + kp.parts - 1) / kp.parts), t_lo = part * per, n_tiles = min(tiles.count - t_lo, per);
+    const int per = max(kp.per_part, kp.by_parts(tiles.count + kp.parts - 1)), t_lo = part * per, n_tiles = min(tiles.count - t_lo, per);
     if (n_tiles <= 0 && part > 0) return;         // (nothing to see at all: part 0 writes it)
     const bool whole = n_tiles == tiles.count;
     // step t takes tile t_lo + t, counted backwards
@@ -266,7 +267,7 @@ __global__ __launch_bounds__(64 * NW, DV <= 128 ? 2 : 1) void scored_tile_kernel
     const int strips = PAGED ? d.page >> 4 : 1, strip_end = (r.n + 15) >> 4;
     auto find_blocks = [&](int t) __attribute__((always_inline)) {
         const int strip = first_key(t) / 16 + (lane & 3);
-        const int blk = kp.block_table[(size_t)b * d.max_blocks + min(strip, strip_end - 1) / strips];
+        const int blk = kp.block_table[(size_t)b * d.max_blocks + d.by_strips(min(strip, strip_end - 1))];
         k_block = strip < strip_end && (unsigned)blk < (unsigned)d.n_blocks ? blk : -1;
     };
     auto load_keys = [&](int t) __attribute__((always_inline)) {
@@ -277,7 +278,7 @@ __global__ __launch_bounds__(64 * NW, DV <= 128 ? 2 : 1) void scored_tile_kernel
             const int blk = __shfl(k_block, j >> 4, 64);
             const size_t unit = (size_t)max(blk, 0) * d.S + s;
             kreg[i] = make_uint4(0, 0, 0, 0);
-            if (16 * piece < d.d_sel) kreg[i] = *reinterpret_cast<const uint4 *>(kp.sel_q8 + (unit * d.page + (strip % strips) * 16 + (j & 15)) * d.d_sel + 16 * piece);
+            if (16 * piece < d.d_sel) kreg[i] = *reinterpret_cast<const uint4 *>(kp.sel_q8 + (unit * d.page + (strip - d.by_strips(strip) * strips) * 16 + (j & 15)) * d.d_sel + 16 * piece);
             k_scale[i] = kp.scales[2 * unit + 1];
         }
     };
@@ -289,7 +290,7 @@ __global__ __launch_bounds__(64 * NW, DV <= 128 ? 2 : 1) void scored_tile_kernel
             const int blk = __shfl(v_block, u / DV, 64);
             const size_t unit = (size_t)max(blk, 0) * d.S + s;
             vreg[i] = make_uint4(0, 0, 0, 0);
-            if (col < d.d_pool && blk >= 0) vreg[i] = *reinterpret_cast<const uint4 *>(kp.pool_q8 + ((unit * strips + strip % strips) * d.d_pool + col) * 16);
+            if (col < d.d_pool && blk >= 0) vreg[i] = *reinterpret_cast<const uint4 *>(kp.pool_q8 + ((unit * strips + strip - d.by_strips(strip) * strips) * d.d_pool + col) * 16);
             v_scale[i] = kp.scales[2 * unit];
         }
     };
@@ -618,40 +619,31 @@ __global__ __launch_bounds__(256) void scored_merge_kernel(const TileParams kp)
     const ServeDims &d = kp.d;
     const int lane = threadIdx.x & 63, u = blockIdx.x / (BM / 4);
     const int k = (blockIdx.x % (BM / 4)) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int x = kp.items - 1 - u / d.S, s = u % d.S;
+    const int y = d.by_S(u), x = kp.items - 1 - y, s = u - y * d.S;
     int item0;
     const int b = request_of_item(kp.q_start, d, x, lane, item0);
     const Request r = make_request(kp.q_start, kp.seq_len, kp.prefix_len, b, d.T, d.max_blocks * d.page);
     const int columns = r.rows * d.hps, c_first = (x - item0) * BM, c = c_first + k;
     if (x < item0 || c >= columns || columns < kp.least) return;
     const Tiles tiles = make_tiles(d, kp.rule, r, c_first, columns);
-    const int per = max(kp.per_part, (tiles.count + kp.parts - 1) / kp.parts);
+    const int per = max(kp.per_part, kp.by_parts(tiles.count + kp.parts - 1));
     if (tiles.count <= per) return;               // one part: it has written the output
     const int parts = (tiles.count + per - 1) / per;
     const float *src = kp.part + ((size_t)u * kp.parts * BM + k) * (DV + 2);
-    constexpr size_t STEP = (size_t)BM * (DV + 2);
-    float m = -INFINITY, l = 0.f, sum[V];
-    for (int p = 0; p < parts; ++p) m = fmaxf(m, src[p * STEP]);
-#pragma unroll
-    for (int v = 0; v < V; ++v) sum[v] = 0.f;
-#pragma unroll 4
-    for (int p = 0; p < parts; ++p) {
-        const float *part = src + p * STEP;
-        const float f = part[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(part[0] - m);
-        l = fmaf(part[1], f, l);
-#pragma unroll
-        for (int v = 0; v < V; ++v) sum[v] = fmaf(part[2 + lane + 64 * v], f, sum[v]);
-    }
+    float m, l, sum[V];
+    merge_parts<V>(src, (size_t)BM * (DV + 2), parts, lane, m, l, sum);
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int row = c / d.hps, head = s * d.hps + (c - row * d.hps);
+    const int row = d.by_hps(c), head = s * d.hps + (c - row * d.hps);
     const size_t at = (size_t)(r.first + row) * d.H + head;
     bool fine = true;
+    T o[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const float o = sum[v] * inv;
-        fine = fine && fabsf(o) < INFINITY;
-        if (lane + 64 * v < d.d_pool) ((T *)kp.O + at * d.d_pool)[lane + 64 * v] = from_float<T>(o);
+        const float y = sum[v] * inv;
+        fine = fine && fabsf(y) < INFINITY;
+        o[v] = from_float<T>(y);
     }
+    if (lane * V < d.d_pool) __builtin_memcpy(__builtin_assume_aligned((T *)kp.O + at * d.d_pool + lane * V, V * sizeof(T)), o, V * sizeof(T));     // (V divides 8)
     if (kp.lse != nullptr && lane == 0) kp.lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(!fine) != 0, 0)) row_again<E, DV, PAGED>(kp, r, b, s, c, lane);
 }
@@ -698,7 +690,7 @@ template <bool PAGED> hipError_t launch(const ScoredArgs &a, int least, hipStrea
 {
     const Plan p = make_plan(a.d, PAGED);
     const TileParams kp{a.Q, a.SEL, a.POOL, a.O, a.lse, a.q_start, a.seq_len, a.prefix_len, a.block_table, a.slopes, a.sel_q8, a.pool_q8, a.scales, a.d,
-                        score_rule(a.d), p.items, least, p.parts, p.per_part, a.part};
+                        score_rule(a.d), p.items, least, p.parts, p.per_part, FastDiv(p.parts), a.part};
     if (a.d.dtype == LCA_F16) run_widths<_Float16, PAGED>(kp, st);
     else run_widths<__bf16, PAGED>(kp, st);
     return hipGetLastError();

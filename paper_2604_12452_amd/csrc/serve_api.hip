@@ -11,6 +11,7 @@ namespace {
 
 using lca::check_ptr;
 using lca::fail;
+using lca::FastDiv;
 using lca::ServeDims;
 
 enum { TABLES = 1, CACHE = 2, ATTENTION = 4 };           // what a call reads of the descriptor
@@ -58,6 +59,7 @@ lca_status make_dims(const lca_serve_desc *desc, int what, ServeDims &d)
         if (desc->d_pool % 16 || desc->d_sel % 16 || desc->d_pool > 256 || desc->d_sel > 256)
             return fail(LCA_ERR_UNSUPPORTED, "the 8-bit cache takes widths that are multiples of 16 up to 256");
     }
+    d.by_hps = FastDiv(d.hps); d.by_S = FastDiv(d.S); d.by_page = FastDiv(d.page); d.by_strips = FastDiv(d.page / 16);
     const int capacity = (int)std::min<int64_t>(std::max<int64_t>((int64_t)desc->max_blocks * desc->page, 0), 1 << 30);
     d.max_q = desc->max_q == 0 || desc->max_q > desc->T ? desc->T : desc->max_q;
     d.max_kv = desc->max_kv == 0 || desc->max_kv > capacity ? capacity : desc->max_kv;

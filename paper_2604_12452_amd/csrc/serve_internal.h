@@ -7,12 +7,30 @@
 
 namespace lca {
 
+// x / d for 0 <= x < 2^31 by one multiplication: with s = ceil(log2 d) and mul = ceil(2^(31 + s) / d), mul d exceeds 2^(31 + s)
+// by less than d <= 2^s, which x < 2^31 keeps below one quotient.  (A division of the ALU's own is some thirty dependent
+// instructions, and a short call has a dozen.)
+struct FastDiv {
+    unsigned mul, shift;                          // mul = 0: d = 1
+    FastDiv() = default;
+    explicit FastDiv(int d) : mul(0), shift(0)
+    {
+        if (d <= 1) return;
+        unsigned s = 0;
+        while ((1ull << s) < (unsigned long long)d) ++s;
+        mul = (unsigned)(((1ull << (31 + s)) + d - 1) / d);
+        shift = s - 1;
+    }
+    __device__ __forceinline__ int operator()(int x) const { return mul == 0 ? x : (int)(__umulhi((unsigned)x, mul) >> shift); }
+};
+
 // A validated lca_serve_desc; rows resolved, hints resolved (max_kv <= max_blocks * page, max_q <= T).
 struct ServeDims {
     int B, T, H, S, hps, d_pool, d_sel, dtype;
     int page, n_blocks, max_blocks, max_q, max_kv, window;
     float scale, softcap;
     size_t q_row, sel_row, pool_row;
+    FastDiv by_hps, by_S, by_page, by_strips;     // strips: page / 16
 };
 
 struct TablesArgs {

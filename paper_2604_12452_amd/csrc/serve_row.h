@@ -47,12 +47,13 @@ template <typename T> struct PagedSource {
     const uint8_t *sel_q8, *pool_q8;
     const float *scales;
     int page, n_blocks, S, s, d_sel, d_pool;
-    __device__ __forceinline__ int block(int key) const { return table[key / page]; }
+    FastDiv by_page;
+    __device__ __forceinline__ int block(int key) const { return table[by_page(key)]; }
     __device__ __forceinline__ bool has(int key) const { return (unsigned)block(key) < (unsigned)n_blocks; }
     __device__ __forceinline__ float dot(const T *q, int key, int d) const
     {
         const size_t unit = (size_t)block(key) * S + s;
-        const uint8_t *k = sel_q8 + (unit * page + key % page) * d_sel;
+        const uint8_t *k = sel_q8 + (unit * page + key - by_page(key) * page) * d_sel;
         float sum = 0.f;
         for (int c = 0; c < d; c += 8) {
             T qv[8];
@@ -66,10 +67,47 @@ template <typename T> struct PagedSource {
     __device__ __forceinline__ float value(int key, int c, int d) const
     {
         const size_t unit = (size_t)block(key) * S + s;
-        const int at = key % page;
+        const int at = key - by_page(key) * page;
         return decode_e4m3(pool_q8[((unit * (page >> 4) + (at >> 4)) * d + c) * 16 + (at & 15)]) * scales[2 * unit];
     }
 };
+
+// A column's partial results [max (base 2), sum, 64 V outputs], `step` floats apart, joined by one wavefront: each 16 lanes take
+// every fourth, 4 V outputs a lane, and are added up by exchanges; lane l ends with outputs l V .. l V + V - 1.
+template <int V> __device__ __forceinline__ void merge_parts(const float *src, size_t step, int parts, int lane, float &m, float &l, float (&out)[V])
+{
+    const int q4 = lane >> 4, first = (lane & 15) * 4 * V;
+    m = -INFINITY;
+    for (int p = lane; p < parts; p += 64) m = fmaxf(m, src[p * step]);
+    m = lanes::over_group<64>(m, lanes::Max());
+    float sum[4 * V];
+    l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4 * V; ++i) sum[i] = 0.f;
+#pragma unroll 2
+    for (int p = q4; p < parts; p += 4) {
+        const float *x = src + p * step;
+        const float f = x[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[0] - m);
+        l = fmaf(x[1], f, l);
+#pragma unroll
+        for (int i = 0; i < 4 * V; i += 2) {
+            const float2 y = *reinterpret_cast<const float2 *>(x + 2 + first + i);
+            sum[i] = fmaf(y.x, f, sum[i]);
+            sum[i + 1] = fmaf(y.y, f, sum[i + 1]);
+        }
+    }
+    l = lanes::across32(lanes::across16(l, lanes::Sum()), lanes::Sum());
+#pragma unroll
+    for (int i = 0; i < 4 * V; ++i) sum[i] = lanes::across32(lanes::across16(sum[i], lanes::Sum()), lanes::Sum());
+    // lane l has columns first + 0 .. 4 V - 1 of its l & 15; its own are those of lane l / 4, from (l & 3) V on
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        float y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[k] = __shfl(sum[k * V + v], lane >> 2, 64);
+        out[v] = (lane & 3) == 0 ? y[0] : (lane & 3) == 1 ? y[1] : (lane & 3) == 2 ? y[2] : y[3];
+    }
+}
 
 // Row at position i (< r.n) of request r: its output to O (d_pool elements) and lse (may be NULL).  All 64 lanes take
 // part, everything but the lane is the same for all of them.  NV: columns per lane (64 NV >= d_pool).
