@@ -2,7 +2,7 @@
 // prompts over the paged 8-bit cache (scored_tile_paged.hip).
 //
 // The (row, query head) pairs of a request and KV head are columns, row after row, whatever the number of heads: a wavefront
-// takes 32 of them, a workgroup of four 128, and all of them share the tiles of 64 keys and values in LDS.
+// takes 32 of them, and a workgroup's wavefronts (four, over the cache eight) share the tiles of 64 keys and values in LDS.
 //   S^T[key, column] = K Q^T      32x32x16 MFMAs, A = keys from LDS, B = the queries, in registers throughout
 //   O^T[dv, column] += V^T P^T    A = values, B = P^T = exp2(S^T - m)
 // A lane holds 16 of 32 scores of one column (the lane 32 further the others), so that maxima and sums are the lane's own
@@ -92,8 +92,9 @@ struct TileParams {
     float *part;                                  // their results, [item, KV head, part, BM, DV + 2]
 };
 
-constexpr int NW = 4;                             // wavefronts per workgroup
-constexpr int BM = 32 * NW;                       // columns of an item
+// Wavefronts per workgroup (32 columns each): over the cache eight, so that a tile's codes are converted for 256 columns, unless
+// the width takes the registers of two wavefronts per SIMD.
+constexpr int wavefronts(bool paged, int dv) { return paged && dv <= 128 ? 8 : 4; }
 constexpr int BN = 64;                            // keys of a tile
 constexpr float LAZY = 8.f;                       // where maxima are taken, the reference may lag them this much (base 2)
 // A lane's 16 weights of a half may add up to this: in fp16 none of them is then beyond 65504; fp32 and bf16 end at 2^127.  Past
@@ -121,7 +122,7 @@ __device__ __forceinline__ void copy_1k(unsigned voff, const int4v &rs, unsigned
 
 // The request of work item x (counted from the first): request b's items start at floor(q_start[b] * hps / BM) + b, which leaves
 // each at least as many numbers as it has items; 64 starts are looked at at a time.
-__device__ __forceinline__ int request_of_item(const int32_t *q_start, const ServeDims &d, int x, int lane, int &first)
+template <int BM> __device__ __forceinline__ int request_of_item(const int32_t *q_start, const ServeDims &d, int x, int lane, int &first)
 {
     auto start = [&](int b) __attribute__((always_inline)) { return (int)((long)min(max(q_start[b], 0), d.T) * d.hps / BM) + b; };
     int lo = 0, n = d.B;                          // the request is one of [lo, lo + n): the last that starts at or before x
@@ -139,7 +140,7 @@ __device__ __forceinline__ int request_of_item(const int32_t *q_start, const Ser
 
 // What an item's rows see, in tiles: [0, pre) and [from, ..), numbered one behind the other.
 struct Tiles { int pre, from, count; };
-__device__ __forceinline__ Tiles make_tiles(const ServeDims &d, const ScoreRule &rule, const Request &r, int c_first, int columns)
+template <int BM> __device__ __forceinline__ Tiles make_tiles(const ServeDims &d, const ScoreRule &rule, const Request &r, int c_first, int columns)
 {
     const int lo = max(r.pos0 + d.by_hps(c_first), 0), hi = r.pos0 + d.by_hps(min(c_first + BM - 1, columns - 1));      // positions of its rows
     Tiles t;
@@ -171,19 +172,19 @@ __device__ __forceinline__ void row_again(const TileParams &kp, const Request &r
 }
 
 template <typename E, int DK, int DV, bool PAGED, bool CAP, bool BIAS>
-__global__ __launch_bounds__(64 * NW, DV <= 128 ? 2 : 1) void scored_tile_kernel(const TileParams kp)
+__global__ __launch_bounds__(64 * wavefronts(PAGED, DV), DV <= 128 ? 2 : 1) void scored_tile_kernel(const TileParams kp)
 {
     typedef typename Store<E>::type T;
     typedef E ex8 __attribute__((ext_vector_type(8)));
     typedef E ex4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) ex4 *lds_b64_ptr;
     typedef const __attribute__((address_space(3))) ex8 *lds_b128_ptr;
-    constexpr int NKS = DK / 16, NDV = DV / 32;
+    constexpr int NW = wavefronts(PAGED, DV), BM = 32 * NW, NKS = DK / 16, NDV = DV / 32;
     constexpr int RBK = 2 * DK, RBV = 2 * DV;     // bytes of a row of keys and of values in LDS
     constexpr int RBT = 2 * BN;                   // PAGED: the values lie transposed, a row per column
     constexpr int K_BYTES = BN * RBK, V_BYTES = BN * RBV, V_AT = 2 * K_BYTES;        // two buffers of keys, then two of values
     constexpr int K_COPIES = K_BYTES / 1024 / NW, V_COPIES = BN * RBV / 1024 / NW;
-    static_assert(K_BYTES % (1024 * NW) == 0 && (BN * RBV) % (1024 * NW) == 0, "whole copies");
+    static_assert(PAGED || (K_BYTES % (1024 * NW) == 0 && V_BYTES % (1024 * NW) == 0), "whole copies");
     extern __shared__ __attribute__((aligned(1024))) char lds[];
 
     const ServeDims &d = kp.d;
@@ -192,7 +193,7 @@ __global__ __launch_bounds__(64 * NW, DV <= 128 ? 2 : 1) void scored_tile_kernel
     // one KV head's items follow one another at a distance of S (an XCD sees few heads), the last rows first
     const int u = kp.by_parts((int)blockIdx.x), part = blockIdx.x - u * kp.parts, y = d.by_S(u), x = kp.items - 1 - y, s = u - y * d.S;
     int item0;
-    const int b = request_of_item(kp.q_start, d, x, lane, item0);
+    const int b = request_of_item<BM>(kp.q_start, d, x, lane, item0);
     const Request r = make_request(kp.q_start, kp.seq_len, kp.prefix_len, b, d.T, d.max_blocks * d.page);
     const int columns = r.rows * d.hps, c_first = (x - item0) * BM;
     if (x < item0 || c_first >= columns || columns < kp.least) return;
@@ -204,7 +205,7 @@ __global__ __launch_bounds__(64 * NW, DV <= 128 ? 2 : 1) void scored_tile_kernel
     // positions of the wavefront's and of the item's rows
     const int w_lo = __builtin_amdgcn_readfirstlane(r.pos0 + d.by_hps(min(c_first + 32 * wave, columns - 1)));
     const int w_hi = __builtin_amdgcn_readfirstlane(r.pos0 + d.by_hps(min(c_first + 32 * wave + 31, columns - 1)));
-    const Tiles tiles = make_tiles(d, kp.rule, r, c_first, columns);
+    const Tiles tiles = make_tiles<BM>(d, kp.rule, r, c_first, columns);
     const int per = max(kp.per_part, kp.by_parts(tiles.count + kp.parts - 1)), t_lo = part * per, n_tiles = min(tiles.count - t_lo, per);
     if (n_tiles <= 0 && part > 0) return;         // (nothing to see at all: part 0 writes it)
     const bool whole = n_tiles == tiles.count;
@@ -259,7 +260,8 @@ __global__ __launch_bounds__(64 * NW, DV <= 128 ? 2 : 1) void scored_tile_kernel
     };
     // The cache: a thread takes 16 codes of a key, 16 tokens of a column; a tile's blocks are looked up a step before its
     // keys are loaded, its values follow a step behind.
-    constexpr int K_PIECES = PAGED ? BN * DK / 16 / (64 * NW) : 1, V_PIECES = PAGED ? 4 * DV / (64 * NW) : 1;
+    constexpr int K_TOTAL = BN * DK / 16, V_TOTAL = 4 * DV, THREADS = 64 * NW;
+    constexpr int K_PIECES = PAGED ? (K_TOTAL + THREADS - 1) / THREADS : 1, V_PIECES = PAGED ? (V_TOTAL + THREADS - 1) / THREADS : 1;
     uint4 kreg[K_PIECES], vreg[V_PIECES];
     float k_scale[K_PIECES], v_scale[V_PIECES];
     int k_block = -1, v_block = -1;               // lane: block of strip lane & 3 of the next tile of keys and of values to be loaded
@@ -274,11 +276,11 @@ __global__ __launch_bounds__(64 * NW, DV <= 128 ? 2 : 1) void scored_tile_kernel
         const int strip0 = first_key(t) / 16;
 #pragma unroll
         for (int i = 0; i < K_PIECES; ++i) {
-            const int u = i * 64 * NW + tid, j = u / (DK / 16), piece = u % (DK / 16), strip = strip0 + (j >> 4);
+            const int u = i * THREADS + tid, j = u / (DK / 16), piece = u % (DK / 16), strip = strip0 + (j >> 4);
             const int blk = __shfl(k_block, j >> 4, 64);
             const size_t unit = (size_t)max(blk, 0) * d.S + s;
             kreg[i] = make_uint4(0, 0, 0, 0);
-            if (16 * piece < d.d_sel) kreg[i] = *reinterpret_cast<const uint4 *>(kp.sel_q8 + (unit * d.page + (strip - d.by_strips(strip) * strips) * 16 + (j & 15)) * d.d_sel + 16 * piece);
+            if (u < K_TOTAL && 16 * piece < d.d_sel) kreg[i] = *reinterpret_cast<const uint4 *>(kp.sel_q8 + (unit * d.page + (strip - d.by_strips(strip) * strips) * 16 + (j & 15)) * d.d_sel + 16 * piece);
             k_scale[i] = kp.scales[2 * unit + 1];
         }
     };
@@ -286,11 +288,11 @@ __global__ __launch_bounds__(64 * NW, DV <= 128 ? 2 : 1) void scored_tile_kernel
         const int strip0 = first_key(t) / 16;
 #pragma unroll
         for (int i = 0; i < V_PIECES; ++i) {
-            const int u = i * 64 * NW + tid, strip = strip0 + u / DV, col = u % DV;
+            const int u = i * THREADS + tid, strip = strip0 + u / DV, col = u % DV;
             const int blk = __shfl(v_block, u / DV, 64);
             const size_t unit = (size_t)max(blk, 0) * d.S + s;
             vreg[i] = make_uint4(0, 0, 0, 0);
-            if (col < d.d_pool && blk >= 0) vreg[i] = *reinterpret_cast<const uint4 *>(kp.pool_q8 + ((unit * strips + strip - d.by_strips(strip) * strips) * d.d_pool + col) * 16);
+            if (u < V_TOTAL && col < d.d_pool && blk >= 0) vreg[i] = *reinterpret_cast<const uint4 *>(kp.pool_q8 + ((unit * strips + strip - d.by_strips(strip) * strips) * d.d_pool + col) * 16);
             v_scale[i] = kp.scales[2 * unit];
         }
     };
@@ -298,7 +300,8 @@ __global__ __launch_bounds__(64 * NW, DV <= 128 ? 2 : 1) void scored_tile_kernel
         char *kb = lds + (t & 1) * K_BYTES;
 #pragma unroll
         for (int i = 0; i < K_PIECES; ++i) {
-            const int u = i * 64 * NW + tid, j = u / (DK / 16), piece = u % (DK / 16), m = (j & 32) + pi(j & 31);       // (pi is its own inverse)
+            const int u = i * THREADS + tid, j = u / (DK / 16), piece = u % (DK / 16), m = (j & 32) + pi(j & 31);       // (pi is its own inverse)
+            if (K_TOTAL % THREADS != 0 && u >= K_TOTAL) break;
             *reinterpret_cast<uint4 *>(kb + m * RBK + (((2 * piece) ^ key_swizzle<DK>(m)) << 4)) = convert8<E>(kreg[i].x, kreg[i].y, k_scale[i]);
             *reinterpret_cast<uint4 *>(kb + m * RBK + (((2 * piece + 1) ^ key_swizzle<DK>(m)) << 4)) = convert8<E>(kreg[i].z, kreg[i].w, k_scale[i]);
         }
@@ -308,7 +311,8 @@ __global__ __launch_bounds__(64 * NW, DV <= 128 ? 2 : 1) void scored_tile_kernel
         const int strip0 = first_key(t) / 16;
 #pragma unroll
         for (int i = 0; i < V_PIECES; ++i) {
-            const int u = i * 64 * NW + tid, st = u / DV, col = u % DV, real = r.n - (strip0 + st) * 16;        // tokens of the strip that the request has
+            const int u = i * THREADS + tid, st = u / DV, col = u % DV, real = r.n - (strip0 + st) * 16;        // tokens of the strip that the request has
+            if (V_TOTAL % THREADS != 0 && u >= V_TOTAL) break;
             if (real < 16) {
                 unsigned w[4] = {vreg[i].x, vreg[i].y, vreg[i].z, vreg[i].w};
 #pragma unroll
@@ -550,7 +554,10 @@ __global__ __launch_bounds__(64 * NW, DV <= 128 ? 2 : 1) void scored_tile_kernel
         __syncthreads();
         if (over) flags[wave] = 1;
         __syncthreads();
-        again = __builtin_amdgcn_readfirstlane(flags[0] | flags[1] | flags[2] | flags[3]) != 0;
+        int any = 0;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) any |= flags[w];
+        again = __builtin_amdgcn_readfirstlane(any) != 0;
         if (__builtin_expect(!again, 1)) break;
         __syncthreads();
         m_run = m_seen = -INFINITY;
@@ -615,17 +622,17 @@ template <typename E, int DV, bool PAGED>
 __global__ __launch_bounds__(256) void scored_merge_kernel(const TileParams kp)
 {
     typedef typename Store<E>::type T;
-    constexpr int V = DV / 64;
+    constexpr int V = DV / 64, BM = 32 * wavefronts(PAGED, DV);
     const ServeDims &d = kp.d;
     const int lane = threadIdx.x & 63, u = blockIdx.x / (BM / 4);
     const int k = (blockIdx.x % (BM / 4)) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int y = d.by_S(u), x = kp.items - 1 - y, s = u - y * d.S;
     int item0;
-    const int b = request_of_item(kp.q_start, d, x, lane, item0);
+    const int b = request_of_item<BM>(kp.q_start, d, x, lane, item0);
     const Request r = make_request(kp.q_start, kp.seq_len, kp.prefix_len, b, d.T, d.max_blocks * d.page);
     const int columns = r.rows * d.hps, c_first = (x - item0) * BM, c = c_first + k;
     if (x < item0 || c >= columns || columns < kp.least) return;
-    const Tiles tiles = make_tiles(d, kp.rule, r, c_first, columns);
+    const Tiles tiles = make_tiles<BM>(d, kp.rule, r, c_first, columns);
     const int per = max(kp.per_part, kp.by_parts(tiles.count + kp.parts - 1));
     if (tiles.count <= per) return;               // one part: it has written the output
     const int parts = (tiles.count + per - 1) / per;
@@ -648,25 +655,32 @@ __global__ __launch_bounds__(256) void scored_merge_kernel(const TileParams kp)
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(!fine) != 0, 0)) row_again<E, DV, PAGED>(kp, r, b, s, c, lane);
 }
 
+// The widths kernels are built for: 64 / 64, 128 / 128, 192 / 128, 256 / 256.
+constexpr int width_class(int dk, int dv) { return dk <= 64 && dv <= 64 ? 0 : dk <= 128 && dv <= 128 ? 1 : dk <= 192 && dv <= 128 ? 2 : 3; }
+constexpr int CLASS_DV[4] = {64, 128, 128, 256};
+
 // How a call is split, from its sizes and hints: items of BM columns, and where they alone do not fill the chip their tiles.
 struct Plan { int items, parts, per_part; };
 Plan make_plan(const ServeDims &d, bool paged)
 {
+    const int BM = 32 * wavefronts(paged, CLASS_DV[width_class(d.d_sel, d.d_pool)]);
     Plan p;
     p.items = (int)((long)d.T * d.hps / BM) + d.B;
     const long keys = paged ? d.max_kv : d.max_q;
     const long tiles = std::max<long>(1, ((d.window > 0 ? std::min<long>(keys, (long)d.window + BM) : keys) + BN - 1) / BN);
     const long busy = std::max<long>(1, (long)d.T * d.hps / BM) * d.S;         // items that have work, about
-    const long parts = std::max<long>(1, std::min<long>(512 / busy, tiles / 8));
+    // As many workgroups as run at a time (eight wavefronts: one per CU, four: two), of eight tiles at least.  Chunks of 700 rows over 9000 tokens
+    // and five more, 32 heads over 8: 187 us for 256 workgroups, 202 for 512, 215 for 1024.
+    const long parts = std::max<long>(1, std::min<long>(1024 / (BM / 32) * 2 / busy, tiles / 8));
     p.per_part = (int)((tiles + parts - 1) / parts);
     p.parts = (int)((tiles + p.per_part - 1) / p.per_part);
     return p;
 }
-constexpr int width_class(int dk, int dv) { return dk <= 64 && dv <= 64 ? 0 : dk <= 128 && dv <= 128 ? 1 : dk <= 192 && dv <= 128 ? 2 : 3; }
 
 template <typename E, int DK, int DV, bool PAGED> void run(const TileParams &kp, hipStream_t st)
 {
     constexpr size_t bytes = 2 * (size_t)BN * 2 * (DK + DV);
+    constexpr int NW = wavefronts(PAGED, DV), BM = 32 * NW;
     const unsigned grid = (unsigned)((long)kp.items * kp.d.S * kp.parts);
     const bool cap = kp.rule.cap_log2 > 0.f, bias = kp.slopes != nullptr;
     if (cap && bias) scored_tile_kernel<E, DK, DV, PAGED, true, true><<<grid, 64 * NW, bytes, st>>>(kp);
