@@ -115,9 +115,16 @@ __device__ __forceinline__ unsigned lds_address(const void *p) { return (unsigne
 
 // 64 x 16 bytes from buffer offsets `voff` of the lanes into LDS bytes [at, at + 1024).  Inline assembly because the
 // compiler would make every later LDS read wait for a load into LDS that it knows of; the waits are by hand.
-__device__ __forceinline__ void copy_1k(unsigned voff, const int4v &rs, unsigned at)
+// Up to four of them follow one another: the instruction's offset moves both ends, and the lanes' offsets take it back (they
+// are counted from COPY_ROOM bytes in front of the buffer for that).
+constexpr int COPY_ROOM = 3 * 1024;
+template <int N> __device__ __forceinline__ void copies(const unsigned *voff, const int4v &rs, unsigned at)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(voff), "s"(rs), "s"(at) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(voff[0]), "s"(rs), "s"(at) : "memory");
+    if constexpr (N > 1) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:1024 lds" : : "v"(voff[1]), "s"(rs) : "memory");
+    if constexpr (N > 2) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:2048 lds" : : "v"(voff[2]), "s"(rs) : "memory");
+    if constexpr (N > 3) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:3072 lds" : : "v"(voff[3]), "s"(rs) : "memory");
+    if constexpr (N > 4) copies<N - 4>(voff + 4, rs, at + 4096);
 }
 
 // The request of work item x (counted from the first): request b's items start at floor(q_start[b] * hps / BM) + b, which leaves
@@ -236,27 +243,24 @@ __global__ __launch_bounds__(64 * wavefronts(PAGED, DV), DV <= 128 ? 2 : 1) void
 #pragma unroll
         for (int i = 0; i < K_COPIES; ++i) {      // LDS row m of a block of 32 keys holds key pi(m)
             const int at = ((wave * K_COPIES + i) * 64 + lane) * 16, m = at / RBK, piece = (at % RBK / 16) ^ key_swizzle<DK>(m);
-            k_voff[i] = 8 * piece < d.d_sel ? ((m & 32) + pi(m & 31)) * k_row + 16 * piece : NOWHERE;
+            k_voff[i] = 8 * piece < d.d_sel ? ((m & 32) + pi(m & 31)) * k_row + 16 * piece + COPY_ROOM - (i & 3) * 1024 : NOWHERE;
         }
 #pragma unroll
         for (int i = 0; i < V_COPIES; ++i) {
             const int at = ((wave * V_COPIES + i) * 64 + lane) * 16, m = at / RBV, piece = (at % RBV / 16) ^ value_swizzle<DV>(m);
-            v_voff[i] = 8 * piece < d.d_pool ? m * v_row + 16 * piece : NOWHERE;
+            v_voff[i] = 8 * piece < d.d_pool ? m * v_row + 16 * piece + COPY_ROOM - (i & 3) * 1024 : NOWHERE;
         }
     }
-    auto copy_keys = [&](int t) __attribute__((always_inline)) {
-        const int j0 = first_key(t), rows = min(r.n - j0, BN) - 1;             // rows behind the tile's first, up to the document's end
-        const unsigned long long at = (unsigned long long)k_base + (size_t)j0 * k_row;
-        const int4v rs = int4v{(int)(unsigned)at, (int)((unsigned)(at >> 32) & 0xFFFFu), (int)(rows * k_row + 2 * d.d_sel), RSRC_WORD3};
-#pragma unroll
-        for (int i = 0; i < K_COPIES; ++i) copy_1k(k_voff[i], rs, lds0 + (t & 1) * K_BYTES + (wave * K_COPIES + i) * 1024);
+    // tile of keys j0 .. into buffer t & 1; `rows` of it lie behind the first
+    auto copy_keys = [&](int t, int j0, int rows) __attribute__((always_inline)) {
+        const unsigned long long at = (unsigned long long)k_base + (size_t)j0 * k_row - COPY_ROOM;
+        const int4v rs = int4v{(int)(unsigned)at, (int)((unsigned)(at >> 32) & 0xFFFFu), (int)(rows * k_row + 2 * d.d_sel + COPY_ROOM), RSRC_WORD3};
+        copies<K_COPIES>(k_voff, rs, lds0 + (t & 1) * K_BYTES + wave * K_COPIES * 1024);
     };
-    auto copy_values = [&](int t) __attribute__((always_inline)) {
-        const int j0 = first_key(t), rows = min(r.n - j0, BN) - 1;
-        const unsigned long long at = (unsigned long long)v_base + (size_t)j0 * v_row;
-        const int4v rs = int4v{(int)(unsigned)at, (int)((unsigned)(at >> 32) & 0xFFFFu), (int)(rows * v_row + 2 * d.d_pool), RSRC_WORD3};
-#pragma unroll
-        for (int i = 0; i < V_COPIES; ++i) copy_1k(v_voff[i], rs, lds0 + V_AT + (t & 1) * V_BYTES + (wave * V_COPIES + i) * 1024);
+    auto copy_values = [&](int t, int j0, int rows) __attribute__((always_inline)) {
+        const unsigned long long at = (unsigned long long)v_base + (size_t)j0 * v_row - COPY_ROOM;
+        const int4v rs = int4v{(int)(unsigned)at, (int)((unsigned)(at >> 32) & 0xFFFFu), (int)(rows * v_row + 2 * d.d_pool + COPY_ROOM), RSRC_WORD3};
+        copies<V_COPIES>(v_voff, rs, lds0 + V_AT + (t & 1) * V_BYTES + wave * V_COPIES * 1024);
     };
     // The cache: a thread takes 16 codes of a key, 16 tokens of a column; a tile's blocks are looked up a step before its
     // keys are loaded, its values follow a step behind.
@@ -420,11 +424,11 @@ __global__ __launch_bounds__(64 * wavefronts(PAGED, DV), DV <= 128 ? 2 : 1) void
             pb[HF][i >> 3][(i & 7) >> 1] = pack(p0, p1);
         }
     };
-    // Whether the whole wavefront sees all of tile t, and all of it has references.
-    auto is_fast = [&](int t) __attribute__((always_inline)) {
-        const int j0 = first_key(t);
-        const bool behind = j0 + BN - 1 <= w_lo;                               // it lies in front of every row
-        bool fast = t + 1 < n_tiles && !unset && !again && ((behind && w_hi - j0 < kp.rule.window) || (j0 + BN - 1 < r.prefix && (BIAS ? behind : w_lo >= 0)));
+    // Whether the whole wavefront sees all of tile t (of keys j0 ..), and all of it has references: it lies in front of every row and
+    // in every row's window, or in the prefix (in front of the rows as well where the distance counts: it is taken without its sign).
+    const int before = w_lo - BN + 1, window_from = w_hi - kp.rule.window, prefix_below = BIAS ? min(r.prefix - BN + 1, before + 1) : w_lo >= 0 ? r.prefix - BN + 1 : 0;
+    auto is_fast = [&](int t, int j0) __attribute__((always_inline)) {
+        bool fast = t + 1 < n_tiles && !unset && !again && ((j0 <= before && j0 > window_from) || j0 < prefix_below);
         if constexpr (PAGED) fast = fast && (valid & 0xF) == 0xF;
         return fast;
     };
@@ -432,7 +436,7 @@ __global__ __launch_bounds__(64 * wavefronts(PAGED, DV), DV <= 128 ? 2 : 1) void
     // (one MFMA each), so that nothing waits for the instruction in front of it: A its logit, with a cap the exponential in it,
     // B the cap's reciprocal, C the weight, D sum and rounding.  Operands are requested RING MFMAs ahead.  Returns the lane's sum.
     constexpr int MFMAS = NKS + 2 * NDV, RING = 3, LAST = CAP ? 3 : 2;
-    auto fast_slot = [&](auto HF, int t) __attribute__((always_inline)) {
+    auto fast_slot = [&](auto HF, int t, int j0) __attribute__((always_inline)) {
         constexpr int hf = decltype(HF)::value;
         constexpr std::integral_constant<int, hf ^ 1> OTHER;
         unsigned kb = k_lane + ((t + hf) & 1) * K_BYTES, vb = v_lane + ((t - 1 + hf) & 1) * V_BYTES;
@@ -442,7 +446,7 @@ __global__ __launch_bounds__(64 * wavefronts(PAGED, DV), DV <= 128 ? 2 : 1) void
 #pragma unroll
         for (int i = 0; i < RING; ++i) ring[i] = request(i);
         float sum[2] = {0.f, 0.f}, x[16];
-        const float top = (CAP ? kp.rule.cap_log2 : 0.f) - m_run, bias = BIAS ? fmaf(slope, (float)(first_key(t) + 32 * hf + 8 * h32 - pos), top) : top;
+        const float top = (CAP ? kp.rule.cap_log2 : 0.f) - m_run, bias = BIAS ? fmaf(slope, (float)(j0 + 32 * hf + 8 * h32 - pos), top) : top;
         LCA_FENCE();
         each<MFMAS>([&](auto I) __attribute__((always_inline)) {
             constexpr int i = decltype(I)::value;
@@ -469,12 +473,12 @@ __global__ __launch_bounds__(64 * wavefronts(PAGED, DV), DV <= 128 ? 2 : 1) void
         asm volatile("" : "+v"(sum[0]), "+v"(sum[1]));
         return sum[0] + sum[1];
     };
-    auto slow_weights = [&](auto HF, int t) __attribute__((always_inline)) {
-        const int j0 = first_key(t) + 32 * HF;
-        if (j0 > w_hi && j0 >= r.prefix) pb[HF][0] = pb[HF][1] = uint4v{0, 0, 0, 0};      // (wave-uniform) no column sees any of it
-        else weights_masked(HF, j0);
+    auto slow_weights = [&](auto HF, int j0) __attribute__((always_inline)) {
+        if (j0 + 32 * HF > w_hi && j0 + 32 * HF >= r.prefix) pb[HF][0] = pb[HF][1] = uint4v{0, 0, 0, 0};      // (wave-uniform) no column sees any of it
+        else weights_masked(HF, j0 + 32 * HF);
     };
     // Between the slots of a tile.
+    int j_next = 0;                               // first key of tile t + 1 (packed rows)
     auto exchange = [&](int t) __attribute__((always_inline)) {
         if constexpr (!PAGED) asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // this wavefront's part of keys t + 1 and values t has landed
         __syncthreads();                                                       // everybody's has, and everybody is done with keys t and values t - 1
@@ -491,8 +495,10 @@ __global__ __launch_bounds__(64 * wavefronts(PAGED, DV), DV <= 128 ? 2 : 1) void
                 load_keys(t + 3);
             }
         } else {
-            if (t + 2 < n_tiles) copy_keys(t + 2);
-            if (t + 1 < n_tiles) copy_values(t + 1);
+            // (only the first tile may end behind the document)
+            if (t + 1 < n_tiles) copy_values(t + 1, j_next, BN - 1);
+            j_next = first_key(t + 2);
+            if (t + 2 < n_tiles) copy_keys(t + 2, j_next, BN - 1);
         }
     };
     constexpr std::integral_constant<int, 0> FIRST;
@@ -514,33 +520,38 @@ __global__ __launch_bounds__(64 * wavefronts(PAGED, DV), DV <= 128 ? 2 : 1) void
                 }
             }
         } else {
-            copy_keys(0);
-            copy_values(0);
-            if (n_tiles > 1) copy_keys(1);
+            const int j0 = first_key(0), rows = min(r.n - j0, BN) - 1;
+            j_next = first_key(1);
+            copy_keys(0, j0, rows);
+            copy_values(0, j0, rows);
+            if (n_tiles > 1) copy_keys(1, j_next, BN - 1);
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         }
         __syncthreads();
         scores(FIRST, 0);
-        for (int t = 0; t < n_tiles; ++t) {
+        for (int t = 0, j0 = first_key(0); t < n_tiles; ++t) {
+            float s0 = 0.f, s1 = 0.f;
             bool calm = true;
 #pragma clang loop unroll(disable)
-            for (; is_fast(t) && calm; ++t) {
-                const float s0 = fast_slot(FIRST, t);
+            for (; is_fast(t, j0) && calm; ++t) {
+                s0 = fast_slot(FIRST, t, j0);
                 exchange(t);
-                const float s1 = fast_slot(SECOND, t), larger = s0 > s1 ? s0 : s1;
+                s1 = fast_slot(SECOND, t, j0);
                 l_run += s0 + s1;
-                over = over || !(s0 <= Limit<E>::value && s1 <= Limit<E>::value);
+                if constexpr (std::is_same<E, _Float16>::value) over = over || !(s0 <= Limit<E>::value && s1 <= Limit<E>::value);
                 calm = __builtin_amdgcn_ballot_w64(!(s0 + s1 <= CALM)) == 0;
-                m_seen = s0 + s1 <= CALM ? -INFINITY : m_run + __builtin_amdgcn_logf(larger);
+                j0 = first_key(t + 1);
                 valid >>= 4;
             }
+            m_seen = s0 + s1 <= CALM ? -INFINITY : m_run + __builtin_amdgcn_logf(s0 > s1 ? s0 : s1);
             if (t > 0) add_values(SECOND, t - 1);
             scores(SECOND, t);
-            slow_weights(FIRST, t);
+            slow_weights(FIRST, j0);
             exchange(t);
             add_values(FIRST, t);
             if (t + 1 < n_tiles) scores(FIRST, t + 1);
-            slow_weights(SECOND, t);
+            slow_weights(SECOND, j0);
+            j0 = first_key(t + 1);
             valid >>= 4;
         }
         add_values(SECOND, n_tiles - 1);
