@@ -68,6 +68,8 @@ struct DecodeParams {
 };
 
 constexpr int TILE = 64;
+// Whether a wavefront needs the registers of two.
+constexpr bool heavy(int dv, int nct) { return dv * nct >= 256; }
 
 // What a request's rows see, in tiles: [0, pre) and [from, to), numbered one behind the other.
 struct Tiles { int pre, from, count; };
@@ -118,7 +120,7 @@ __device__ __forceinline__ bool write_column(const DecodeParams &kp, const Reque
 }
 
 template <typename E, int DK, int DV, int NCT>
-__global__ __launch_bounds__(256, 2) void page_decode_kernel(const DecodeParams kp)
+__global__ __launch_bounds__(256, heavy(DV, NCT) ? 1 : 2) void page_decode_kernel(const DecodeParams kp)
 {
     typedef E ex8 __attribute__((ext_vector_type(8)));
     constexpr int NK = DK / 64, NV = DV / 16, ROW = DV + 4;
@@ -424,8 +426,13 @@ Plan make_plan(const ServeDims &d)
     long keys = d.max_kv;
     if (d.window > 0) keys = std::min<long>(keys, (long)d.window + d.max_q + TILE);
     const long tiles = std::max<long>(1, (keys + TILE - 1) / TILE), units = (long)d.B * d.S * p.groups;
-    long parts = std::max<long>(1, 1024 / units);
-    parts = tiles <= 16 ? 1 : std::min<long>(parts, (tiles + 3) / 4);
+    // Twice the workgroups that run at a time: requests are of different lengths, and the parts of the long ones fill in behind the
+    // short ones (20 requests of up to 9000 tokens, 32 heads over 8: 30 us, 41 with half as many; 4 of 30000 each 48 and 45).  Where a
+    // wavefront needs the registers of two, one for each CU: 8 requests of 16000, 40 heads over one, 23 us, 27 with twice as many, 38 with
+    // four times.  Up to 16 tiles, and up to 64 where there is a workgroup per CU without it, nothing is split and there is nothing to join: 500
+    // tokens, 28 heads over 4, 9.9 us, 11.4 in two parts; 64 requests of up to 1500, 17 us, 25 in two.
+    const long target = heavy(dv, p.nct) ? 256 : 1024;
+    long parts = tiles <= 16 || (units >= 256 && tiles <= 64) ? 1 : std::max<long>(1, std::min<long>(target / units, (tiles + 3) / 4));
     p.per_part = (int)((tiles + parts - 1) / parts);
     p.parts = (int)((tiles + p.per_part - 1) / p.per_part);
     return p;
