@@ -548,3 +548,165 @@ def test_a_serving_loop(graph):
         assert (O[rows:] == 77).all()
         lens = total
         cached.copy_(seq_len)
+
+
+# ---- where it can go wrong ----
+
+def test_packed_many_documents_and_one_long_one():
+    """More documents than lanes look at in one go, most of a token or two, some empty; one document split over its tiles."""
+    rng = np.random.default_rng(40)
+    lens = rng.choice([0, 1, 1, 2, 3], 5000)
+    starts = np.concatenate([[0], np.cumsum(lens)]).tolist()
+    x = [_randn(rng, "bf16", starts[-1], 1, 64) for _ in range(3)]
+    torch, lca, serve = _api()
+    d = serve.Desc(B=5000, T=starts[-1], H=1, S=1, d_pool=64, d_sel=64)
+    O = torch.zeros((starts[-1], 1, 64), dtype=torch.bfloat16, device="cuda")
+    serve.packed_attn(d, *x, _i32(starts), None, None, O, None, serve.alloc_workspace(d))
+    q, k, v = (_f64(t)[:, 0] for t in x)
+    got = _f64(O)[:, 0]
+    for lo, hi in zip(starts[:-1], starts[1:]):
+        want = ref.attend(q[lo:hi], k[lo:hi], v[lo:hi], np.arange(hi - lo), hi - lo, "bf16")
+        _close(got[lo:hi], want[0], want[2], (lo, hi))
+    x = [_randn(rng, "f16", 2600, 1, 64) for _ in range(3)]
+    _check_packed(*x, [0, 2500], "f16", 0.125, dict())
+    _check_packed(*x, [0, 30, 2600], "f16", 0.125, dict(window=900, prefix=100, slopes=True))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("jump", [8.0, 40.0, 300.0])
+def test_packed_far_keys_with_larger_logits_than_near_ones(dtype, jump):
+    """Keys are taken from the rows backwards: blocks of far keys whose logits exceed the near ones' by a few, by tens, and past either type's exponents."""
+    torch, lca, serve = _api()
+    rng = np.random.default_rng(41)
+    T = 700
+    Q, SEL, POOL = (_randn(rng, dtype, T, 1, 64) for _ in range(3))
+    Q[:, :, 0] = 1.0
+    SEL[:, :, 0] = 0.0
+    for lo, hi, share in ((300, 310, 0.5), (130, 131, 1.0), (5, 70, 0.75)):
+        SEL[lo:hi, :, 0] = jump * share
+    _check_packed(Q, SEL, POOL, [0, T], dtype, 1.0, dict())
+
+
+def test_store_and_attention_past_32_bits_of_offset():
+    """A cache of more than 2^32 bytes of codes each: tokens stored in its last blocks, and attended to."""
+    torch, lca, serve = _api()
+    rng = np.random.default_rng(42)
+    page, S, d, n_blocks = 64, 8, 128, 66000
+    desc = serve.Desc(B=2, T=140, H=S, S=S, d_pool=d, d_sel=d, page=page, n_blocks=n_blocks, max_blocks=3, scale=d ** -0.5)
+    sel, pool = (torch.empty(n_blocks * page * S * d, dtype=torch.uint8, device="cuda") for _ in range(2))
+    scales = torch.zeros((n_blocks, S, 2), device="cuda")
+    used = [65999, 3, 65536, 65535]
+    slot = [65999 * page + i for i in range(64)] + [3 * page + i for i in range(6)] + [65536 * page + i for i in range(64)] + [65535 * page + i for i in range(6)]
+    SEL, POOL, Q = (_randn(rng, "bf16", 140, S, d) for _ in range(3))
+    serve.page_store_q8(desc, SEL, POOL, _i32(slot), sel, pool, scales)
+    where = lambda t, shape: torch.stack([t.view(n_blocks, -1)[b].view(shape) for b in used]).cpu().numpy()      # noqa: E731
+    cache = (where(sel, (S, page, d)), where(pool, (S, page // 16, d, 16)), scales[used].cpu().numpy())
+    for i in (1, 3):                                              # (what lies behind the tokens of a block is not defined)
+        cache[0][i][:, 6:] = 0
+        cache[1][i][:, 1:] = 0
+        cache[1][i][:, 0, :, 6:] = 0
+    want = ref.store(*(np.zeros_like(c) for c in cache), _f64(SEL), _f64(POOL), list(range(64)) + list(range(64, 70)) + list(range(128, 192)) + list(range(192, 198)), "bf16")
+    for got, w in zip(cache, want):
+        np.testing.assert_array_equal(got, w)
+    for rows in (1, 70):                                          # (both kernels; the second with every row of the batch)
+        O = torch.zeros((140, S, d), dtype=torch.bfloat16, device="cuda")
+        q_start = [0, rows, 2 * rows]
+        serve.page_attn_q8(desc, Q, _i32(q_start), _i32([70, 70]), None, None, _i32([[65999, 3, -1], [65536, 65535, -1]]), sel, pool, scales, O, None, serve.alloc_workspace(desc))
+        for b in range(2):
+            for s in range(S):
+                k, v, _ = ref.gather(cache[0], cache[1], cache[2].astype(np.float64), [2 * b, 2 * b + 1], 70, s)
+                r = slice(q_start[b], q_start[b + 1])
+                w = ref.attend(_f64(Q[r])[:, s], k, v, 70 - rows + np.arange(rows), 70, "bf16", scale=d ** -0.5)
+                _close(_f64(O[r])[:, s], w[0], w[2], (rows, b, s))
+
+
+@pytest.mark.parametrize("row", [1 << 22, (1 << 23) + 8])
+def test_packed_tokens_far_apart(row):
+    """Strides whose products pass 2^32 bytes: within what a buffer descriptor spans from tile to tile, and beyond it (row by row)."""
+    torch, lca, serve = _api()
+    rng = np.random.default_rng(43)
+    T, d = 270, 64
+    big = torch.empty((T - 1) * row + 3 * d, dtype=torch.float16, device="cuda")
+    x = torch.as_strided(big, (T, 3, d), (row, d, 1))
+    x.copy_(_randn(rng, "f16", T, 3, d))
+    views = [x[:, i:i + 1] for i in range(3)]
+    _check_packed(*views, [0, 200, 270], "f16", 0.125, RULES["prefix"], q_row=row, sel_row=row, pool_row=row)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_attention_over_scales_at_the_ends_of_their_range(dtype):
+    """Blocks whose scales are the smallest and the largest the store writes: every decoded value is one of the type, and so are the products' operands."""
+    rng = np.random.default_rng(44)
+    lens, page, d = [50, 130], 16, 64
+    (sel, pool, scales), table = _fill_cache(rng, lens, page, 2, d, d)
+    lo, hi = ref.RANGE[dtype]
+    scales[..., 1] = 2.0 ** np.where(rng.random(scales.shape[:2]) < 0.5, lo, -8)       # keys: logits of ordinary size
+    scales[..., 0] = 2.0 ** np.where(rng.random(scales.shape[:2]) < 0.5, lo, hi if dtype == "f16" else 100)
+    sel[(sel & 0x7F) == 0x7F] = 0
+    if dtype == "f16":                                                                  # (outputs of the largest scale end at 65504: smaller codes there)
+        pool &= 0xBF
+    for rows in ([1, 3], [40, 70]):
+        _check_paged(rng, rows, lens, 4, 2, d, d, page, dtype, dict(), max_q=max(rows), cache=((sel, pool, scales), table))
+
+
+def test_two_calls_at_once_and_on_other_streams():
+    """The same inputs on the current stream, and on two streams at a time with workspaces of their own: the same bits, every time."""
+    torch, lca, serve = _api()
+    rng = np.random.default_rng(45)
+    rows, lens = [1] * 5 + [80], [900, 40, 3000, 1, 2000, 700]
+    (sel, pool, scales), table = _fill_cache(rng, lens, 32, 2, 128, 128)
+    q, starts = _randn(rng, "bf16", sum(rows), 8, 128), _i32(np.concatenate([[0], np.cumsum(rows)]))
+    d = serve.Desc(B=6, T=sum(rows), H=8, S=2, d_pool=128, d_sel=128, page=32, n_blocks=len(sel), max_blocks=table.shape[1], scale=0.005)
+    dev = [torch.tensor(x, device="cuda") for x in (sel, pool, scales)]
+    args = (d, q, starts, _i32(lens), None, _slopes(8, True), _i32(table), *dev)
+    packed = serve.Desc(B=1, T=1500, H=2, S=1, d_pool=128, d_sel=128, scale=0.09, softcap=20.0)
+    x = [_randn(rng, "bf16", 1500, h, 128) for h in (2, 1, 1)]
+
+    def buffers():
+        return (torch.empty_like(q), torch.empty((sum(rows), 8), device="cuda"), serve.alloc_workspace(d), torch.empty_like(x[0]), torch.empty((1500, 2), device="cuda"),
+                serve.alloc_workspace(packed))
+
+    def call(b, stream=None):
+        serve.page_attn_q8(*args, *b[:3], stream=stream)
+        serve.packed_attn(packed, *x, _i32([0, 1500]) if stream is None else start, None, None, *b[3:], stream=stream)
+    first = buffers()
+    call(first)
+    start = _i32([0, 1500])
+    torch.cuda.synchronize()
+    streams, others = [torch.cuda.Stream() for _ in range(2)], [buffers() for _ in range(2)]
+    for _ in range(5):
+        for b, s in zip(others, streams):
+            call(b, s)
+        torch.cuda.synchronize()
+        for b in others:
+            for i in (0, 1, 3, 4):
+                assert torch.equal(b[i].view(torch.uint8), first[i].view(torch.uint8))
+
+
+def test_two_graphs_that_share_a_workspace():
+    """Recorded with one workspace, replayed one after the other with other calls between: nothing of one call is left for the next."""
+    torch, lca, serve = _api()
+    rng = np.random.default_rng(46)
+    runs = []
+    for lens, H, d in (([2500, 33], 4, 64), ([700, 1900], 8, 128)):
+        (sel, pool, scales), table = _fill_cache(rng, lens, 16, 2, d, d)
+        desc = serve.Desc(B=2, T=2, H=H, S=2, d_pool=d, d_sel=d, page=16, n_blocks=len(sel), max_blocks=table.shape[1], scale=0.01, max_q=1)
+        q, O = _randn(rng, "bf16", 2, H, d), torch.zeros((2, H, d), dtype=torch.bfloat16, device="cuda")
+        runs.append((desc, [q, _i32([0, 1, 2]), _i32(lens), None, None, _i32(table), *(torch.tensor(x, device="cuda") for x in (sel, pool, scales)), O, None]))
+    ws = torch.empty(max(serve.workspace_size(r[0]) for r in runs), dtype=torch.uint8, device="cuda")
+    want, graphs, side = [], [], torch.cuda.Stream()
+    for desc, args in runs:
+        serve.page_attn_q8(desc, *args, ws)
+        torch.cuda.synchronize()
+        want.append(args[-2].clone())
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            serve.page_attn_q8(desc, *args, ws)
+        graphs.append(g)
+    for _ in range(4):
+        for g, (desc, args), w in zip(graphs, runs, want):
+            args[-2].fill_(77)
+            ws.fill_(0xFF)                                        # (NaN wherever something stale would be read)
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(args[-2], w)
