@@ -11,8 +11,8 @@
 //   P^T     row 4 q + r of S^T's block t (of four) is key 16 q + 4 t + r of the 64, so that a lane's sixteen weights
 //           are those of the sixteen tokens whose values it holds.
 // A code becomes a 16-bit element with the block's scale in one conversion of two (exact: powers of two).
-// A wavefront takes every fourth tile of 64 keys of its workgroup's part on its own; the loads of its next tile are
-// issued as soon as the registers of this one are free.  Softmax with a running maximum, sums in fp32 of the
+// A wavefront takes every W-th tile of 64 keys of its workgroup's part on its own (four of them, eight where a workgroup has a request and
+// a CU to itself); the loads of its next tile are issued as soon as the registers of this one are free.  Softmax with a running maximum, sums in fp32 of the
 // weights before they are rounded.  Parts of long requests are joined by page_merge_kernel.
 #include <algorithm>
 
@@ -119,13 +119,13 @@ __device__ __forceinline__ bool write_column(const DecodeParams &kp, const Reque
     return fine;
 }
 
-template <typename E, int DK, int DV, int NCT>
-__global__ __launch_bounds__(256, heavy(DV, NCT) ? 1 : 2) void page_decode_kernel(const DecodeParams kp)
+template <typename E, int DK, int DV, int NCT, int W>
+__global__ __launch_bounds__(64 * W, heavy(DV, NCT) ? 1 : 2) void page_decode_kernel(const DecodeParams kp)
 {
     typedef E ex8 __attribute__((ext_vector_type(8)));
     constexpr int NK = DK / 64, NV = DV / 16, ROW = DV + 4;
-    __shared__ __attribute__((aligned(16))) float outs[4][16][ROW];
-    __shared__ float stats[4][16][2];
+    __shared__ __attribute__((aligned(16))) float outs[W][16][ROW];
+    __shared__ float stats[W][16][2];
 
     const ServeDims &d = kp.d;
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, q4 = lane >> 4;
@@ -223,9 +223,9 @@ __global__ __launch_bounds__(256, heavy(DV, NCT) ? 1 : 2) void page_decode_kerne
             fetch_blocks(x);
             load_keys(x);
             load_values(x);
-            if (x + 4 < hi) fetch_blocks(x + 4);
+            if (x + W < hi) fetch_blocks(x + W);
         }
-        for (; x < hi; x += 4) {
+        for (; x < hi; x += W) {
             const int j0 = tile_at(x) * TILE + 16 * q4;                        // first key of the lane's strip
             const int blk = v_blk;                                            // (its scores are those of the strip whose values it holds)
             // S^T
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(256, heavy(DV, NCT) ? 1 : 2) void page_decode_kerne
                     for (int k = 0; k < 2 * NK; ++k) sacc[ct][t] = mfma_16x16x32(kf[k], qf[ct][k], sacc[ct][t]);
                 }
             }
-            if (x + 4 < hi) load_keys(x + 4);
+            if (x + W < hi) load_keys(x + W);
 
             // does every row see the whole tile?
             const int j_lo = tile_at(x) * TILE, j_hi = j_lo + TILE - 1;
@@ -325,11 +325,11 @@ __global__ __launch_bounds__(256, heavy(DV, NCT) ? 1 : 2) void page_decode_kerne
                     acc[ct][v] = mfma_16x16x32(v1, pb[ct][1], acc[ct][v]);
                 }
             }
-            if (x + 4 < hi) load_values(x + 4);
-            if (x + 8 < hi) fetch_blocks(x + 8);
+            if (x + W < hi) load_values(x + W);
+            if (x + 2 * W < hi) fetch_blocks(x + 2 * W);
         }
 
-        // the four wavefronts' results, 16 columns at a time
+        // the wavefronts' results, 16 columns at a time
         for (int ct = 0; ct < NCT; ++ct) {
             if (c0 + 16 * ct >= columns) break;
             float m_ct = 0.f, l_ct = 0.f;
@@ -345,40 +345,39 @@ __global__ __launch_bounds__(256, heavy(DV, NCT) ? 1 : 2) void page_decode_kerne
             if (q4 == 0) { stats[wave][col][0] = m_ct; stats[wave][col][1] = l_ct; }
             __syncthreads();
             {
-                // sixteen lanes take a column, DV / 16 outputs each
-                constexpr int N = DV / 16;
-                const int k = wave * 4 + q4, column = c0 + 16 * ct + k, first = col * N;
-                float m = -INFINITY, l = 0.f, sum[N], f[4];
+                // 4 W lanes take a column, N outputs each
+                constexpr int LANES = 4 * W, N = DV / LANES;
+                const int k = tid / LANES, column = c0 + 16 * ct + k, first = (tid % LANES) * N;
+                float m = -INFINITY, l = 0.f, sum[N], f[W];
 #pragma unroll
-                for (int w = 0; w < 4; ++w) m = fmaxf(m, stats[w][k][0]);
+                for (int w = 0; w < W; ++w) m = fmaxf(m, stats[w][k][0]);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
+                for (int w = 0; w < W; ++w) {
                     f[w] = stats[w][k][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stats[w][k][0] - m);
                     l = fmaf(stats[w][k][1], f[w], l);
                 }
 #pragma unroll
                 for (int v = 0; v < N; ++v) sum[v] = 0.f;
 #pragma unroll
-                for (int w = 0; w < 4; ++w)
+                for (int w = 0; w < W; ++w) {
+                    float y[N];
+                    __builtin_memcpy(y, __builtin_assume_aligned(&outs[w][k][first], 4 * (N < 4 ? N : 4)), 4 * N);
 #pragma unroll
-                    for (int v = 0; v < N; v += 4) {
-                        const floatx4 y = *reinterpret_cast<const floatx4 *>(&outs[w][k][first + v]);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) sum[v + i] = fmaf(y[i], f[w], sum[v + i]);
-                    }
+                    for (int v = 0; v < N; ++v) sum[v] = fmaf(y[v], f[w], sum[v]);
+                }
                 if (whole) {
                     const bool fine = column >= columns || write_column<E, N>(kp, r, s, column, first, sum, l, m);
                     unsigned long long odd = __builtin_amdgcn_ballot_w64(!fine);
                     while (__builtin_expect(odd != 0, 0)) {
-                        const int g = __builtin_ctzll(odd) >> 4;
-                        row_again<E, DV>(kp, r, b, s, c0 + 16 * ct + wave * 4 + g, lane);
-                        odd &= ~(0xFFFFull << (16 * g));
+                        const int g = __builtin_ctzll(odd) / LANES;
+                        row_again<E, DV>(kp, r, b, s, c0 + 16 * ct + wave * (64 / LANES) + g, lane);
+                        odd &= ~(((1ull << LANES) - 1) << (LANES * g));
                     }
                 } else {
                     float *dst = kp.part + (((size_t)unit * kp.parts + part) * 16 * NCT + 16 * ct + k) * (DV + 2);
 #pragma unroll
                     for (int v = 0; v < N; v += 2) *reinterpret_cast<float2 *>(dst + 2 + first + v) = float2{sum[v], sum[v + 1]};
-                    if (col == 0) *reinterpret_cast<float2 *>(dst) = float2{m, l};
+                    if (first == 0) *reinterpret_cast<float2 *>(dst) = float2{m, l};
                 }
             }
             __syncthreads();
@@ -411,7 +410,7 @@ __global__ __launch_bounds__(256) void page_merge_kernel(const DecodeParams kp)
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(!fine) != 0, 0)) row_again<E, DV>(kp, r, b, s, column, lane);
 }
 
-struct Plan { int nct, groups, parts, per_part; };
+struct Plan { int nct, groups, parts, per_part, waves; };
 
 // How a call is split, from its sizes and hints.
 Plan make_plan(const ServeDims &d)
@@ -433,24 +432,29 @@ Plan make_plan(const ServeDims &d)
     // tokens, 28 heads over 4, 9.9 us, 11.4 in two parts; 64 requests of up to 1500, 17 us, 25 in two.
     const long target = heavy(dv, p.nct) ? 256 : 1024;
     long parts = tiles <= 16 || (units >= 256 && tiles <= 64) ? 1 : std::max<long>(1, std::min<long>(target / units, (tiles + 3) / 4));
+    // Eight wavefronts where all of them run at once and nothing is split: 500 tokens 9.1 us with four, 8.6 with eight; where there are more
+    // workgroups than CUs (64 requests of up to 1500) 17 and 21, where parts are joined (one request of 2000) 11.2 and 12.2.
+    p.waves = !heavy(dv, p.nct) && parts == 1 && units <= 256 && tiles > 4 ? 8 : 4;
     p.per_part = (int)((tiles + parts - 1) / parts);
     p.parts = (int)((tiles + p.per_part - 1) / p.per_part);
     return p;
 }
 
-template <typename E, int DK, int DV, int NCT> void run(const DecodeParams &kp, hipStream_t st)
+template <typename E, int DK, int DV, int NCT> void run(const DecodeParams &kp, const Plan &p, hipStream_t st)
 {
     const long units = (long)kp.d.B * kp.d.S * kp.groups;
-    page_decode_kernel<E, DK, DV, NCT><<<(unsigned)(units * kp.parts), 256, 0, st>>>(kp);
+    if constexpr (!heavy(DV, NCT))
+        if (p.waves == 8) return page_decode_kernel<E, DK, DV, NCT, 8><<<(unsigned)units, 512, 0, st>>>(kp);          // (one part)
+    page_decode_kernel<E, DK, DV, NCT, 4><<<(unsigned)(units * kp.parts), 256, 0, st>>>(kp);
     if (kp.parts > 1) page_merge_kernel<E, DV, NCT><<<(unsigned)(units * 4 * NCT), 256, 0, st>>>(kp);
 }
 template <typename E, int DK, int DV> void run_columns(const DecodeParams &kp, const Plan &p, hipStream_t st)
 {
     if constexpr (DV == 64)
-        if (p.nct == 4) return run<E, DK, DV, 4>(kp, st);
+        if (p.nct == 4) return run<E, DK, DV, 4>(kp, p, st);
     if constexpr (DV <= 128)
-        if (p.nct == 2) return run<E, DK, DV, 2>(kp, st);
-    run<E, DK, DV, 1>(kp, st);
+        if (p.nct == 2) return run<E, DK, DV, 2>(kp, p, st);
+    run<E, DK, DV, 1>(kp, p, st);
 }
 
 template <typename E> void run_widths(const DecodeParams &kp, const Plan &p, hipStream_t st)

@@ -5,8 +5,11 @@
 // of numbers >= 0 that matter up to a limit only (T, the pool), so they saturate one above it and stay in 32 bits.
 // Tokens: each finds its request among the starts and writes its slot, position and request; the first token of a new
 // block also writes the block table, so that nothing walks the requests' blocks one after another.
-// What bounds it is latency (a decode step moves a kilobyte): one launch where one workgroup takes the tokens along,
-// two where there are many.
+// What bounds it is latency (a decode step moves a kilobyte), so there is one launch: every workgroup takes the sums of all requests
+// for itself, into LDS, and then 1024 tokens (1000 requests, 131072 rows: 7 us, 9 in two launches).  Two launches are left for more requests than LDS
+// holds, and for a free_left that is free_count itself, which the workgroups behind the first would still read.
+#include <algorithm>
+
 #include "serve_internal.h"
 
 namespace lca {
@@ -41,12 +44,12 @@ template <int WAVES> __device__ __forceinline__ int scan_up_to(int v, int limit,
     return min(v + before, limit);
 }
 
-// A token's slot and request: t < T, b its request or -1.
-__device__ __forceinline__ void write_token(const TablesParams &kp, int t, int b, int first)
+// A token's slot and request: t < T, b its request (its first row, its base) or -1.
+__device__ __forceinline__ void write_token(const TablesParams &kp, int t, int b, int first, int base)
 {
     int slot = -1, position = 0;
     if (b >= 0) {
-        const int cached = max(kp.cached_len[b], 0), base = kp.base[b];
+        const int cached = max(kp.cached_len[b], 0);
         position = (int)((unsigned)cached + (unsigned)(t - first));
         if (base != REFUSED) {
             const int col = kp.by_page(position), have = kp.by_page(cached + kp.page - 1);
@@ -66,14 +69,14 @@ __device__ __forceinline__ void write_token(const TablesParams &kp, int t, int b
     kp.request[t] = b;
 }
 
-template <int WAVES, bool TOKENS>
-__global__ __launch_bounds__(WAVES * 64) void tables_requests_kernel(const TablesParams kp)
+// The sums over all requests by one workgroup; put(b, rows up to and including b, seq_len, base) for each, the blocks taken returned to thread 0 as
+// what is left.
+template <int WAVES, typename Put> __device__ __forceinline__ int take_requests(const TablesParams &kp, int *lds, int tid, Put &&put)
 {
-    __shared__ int lds[WAVES];
-    const int tid = threadIdx.x, T1 = kp.T + 1, P1 = kp.n_blocks + 1;
+    __shared__ int carry[2];
+    const int T1 = kp.T + 1, P1 = kp.n_blocks + 1;
     const int free = min(max(kp.free_count[0], 0), kp.n_blocks);
     int rows = 0, blocks = 0, taken = 0;          // of the requests in front of this round
-    if (tid == 0) kp.q_start[0] = 0;
     for (int b0 = 0; b0 < kp.B; b0 += WAVES * 64) {
         const int b = b0 + tid;
         const bool real = b < kp.B;
@@ -86,15 +89,9 @@ __global__ __launch_bounds__(WAVES * 64) void tables_requests_kernel(const Table
         const int need = fits ? min(kp.by_page((int)total + kp.page - 1) - have, P1) : 0;
         const int upto = min(scan_up_to<WAVES>(need, P1, lds, tid) + blocks, P1);
         const bool ok = fits && (need == 0 || upto <= free);
-        if (real) {
-            kp.q_start[b + 1] = min(end, kp.T);
-            kp.seq_len[b] = ok ? (int)total : 0;
-            kp.base[b] = ok ? max(free - 1 - (upto - need), 0) : REFUSED;      // (needs none: any number but REFUSED)
-        }
+        if (real) put(b, min(end, kp.T), ok ? (int)total : 0, ok ? max(free - 1 - (upto - need), 0) : REFUSED);      // (needs none: any base but REFUSED)
         if (ok && need > 0) taken = upto;
-        // the last thread's sums go to all for the next round
-        if (kp.B > b0 + WAVES * 64) {
-            __shared__ int carry[2];
+        if (kp.B > b0 + WAVES * 64) {             // the last thread's sums go to all for the next round
             if (tid == WAVES * 64 - 1) { carry[0] = end; carry[1] = upto; }
             __syncthreads();
             rows = carry[0];
@@ -110,14 +107,46 @@ __global__ __launch_bounds__(WAVES * 64) void tables_requests_kernel(const Table
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) taken = max(taken, lds[w]);
     }
-    if (tid == 0) kp.free_left[0] = free - taken;
-    if constexpr (TOKENS) {
-        __syncthreads();                          // (the workgroup's own writes to q_start and base)
-        for (int t = tid; t < kp.T; t += WAVES * 64) {
-            const int b = request_of(kp.q_start, kp.B, t);
-            write_token(kp, t, b, b >= 0 ? kp.q_start[b] : 0);
-        }
+    return free - taken;
+}
+
+// Up to MOST requests, whose starts and bases stay in LDS; each workgroup every gridDim.x-th WAVES * 64 tokens.
+template <int WAVES, int MOST> __global__ __launch_bounds__(WAVES * 64) void tables_kernel(const TablesParams kp)
+{
+    __shared__ int lds[WAVES], start[MOST + 1], base[MOST];
+    const int tid = threadIdx.x;
+    const bool first = blockIdx.x == 0;
+    if (tid == 0) {
+        start[0] = 0;
+        if (first) kp.q_start[0] = 0;
     }
+    const int left = take_requests<WAVES>(kp, lds, tid, [&](int b, int end, int len, int at) {
+        start[b + 1] = end;
+        base[b] = at;
+        if (first) {
+            kp.q_start[b + 1] = end;
+            kp.seq_len[b] = len;
+        }
+    });
+    if (first && tid == 0) kp.free_left[0] = left;
+    __syncthreads();
+    for (int t = blockIdx.x * (WAVES * 64) + tid; t < kp.T; t += gridDim.x * (WAVES * 64)) {
+        const int b = request_of(start, kp.B, t);
+        write_token(kp, t, b, b >= 0 ? start[b] : 0, b >= 0 ? base[b] : 0);
+    }
+}
+
+__global__ __launch_bounds__(1024) void tables_requests_kernel(const TablesParams kp)
+{
+    __shared__ int lds[16];
+    const int tid = threadIdx.x;
+    if (tid == 0) kp.q_start[0] = 0;
+    const int left = take_requests<16>(kp, lds, tid, [&](int b, int end, int len, int at) {
+        kp.q_start[b + 1] = end;
+        kp.seq_len[b] = len;
+        kp.base[b] = at;
+    });
+    if (tid == 0) kp.free_left[0] = left;
 }
 
 __global__ __launch_bounds__(256) void tables_tokens_kernel(const TablesParams kp)
@@ -125,7 +154,7 @@ __global__ __launch_bounds__(256) void tables_tokens_kernel(const TablesParams k
     const int t = blockIdx.x * 256 + threadIdx.x;
     if (t >= kp.T) return;
     const int b = request_of(kp.q_start, kp.B, t);
-    write_token(kp, t, b, b >= 0 ? kp.q_start[b] : 0);
+    write_token(kp, t, b, b >= 0 ? kp.q_start[b] : 0, b >= 0 ? kp.base[b] : 0);
 }
 
 struct ReleaseParams {
@@ -180,13 +209,16 @@ hipError_t launch_page_tables(const TablesArgs &a, hipStream_t st)
     const ServeDims &d = a.d;
     const TablesParams kp{a.cached_len, a.new_len, a.free_list, a.free_count, a.free_left, a.block_table, a.q_start, a.seq_len, a.slot, a.position, a.request,
                           a.base, d.B, d.T, d.page, d.n_blocks, d.max_blocks, d.by_page};
-    if (d.T <= 4096) {
-        if (d.B <= 64 && d.T <= 256) tables_requests_kernel<1, true><<<1, 64, 0, st>>>(kp);
-        else tables_requests_kernel<16, true><<<1, 1024, 0, st>>>(kp);
-        return hipGetLastError();
+    constexpr int MOST = 4096;
+    const bool in_place = a.free_left == a.free_count;
+    if (d.B <= 64 && d.T <= 256) {
+        tables_kernel<1, 64><<<1, 64, 0, st>>>(kp);
+    } else if (d.B <= MOST && (!in_place || d.T <= 4096)) {
+        tables_kernel<16, MOST><<<in_place ? 1 : (unsigned)std::max(1, (d.T + 1023) / 1024), 1024, 0, st>>>(kp);
+    } else {
+        tables_requests_kernel<<<1, 1024, 0, st>>>(kp);
+        if (d.T > 0) tables_tokens_kernel<<<(unsigned)((d.T + 255) / 256), 256, 0, st>>>(kp);
     }
-    tables_requests_kernel<16, false><<<1, 1024, 0, st>>>(kp);
-    tables_tokens_kernel<<<(unsigned)((d.T + 255) / 256), 256, 0, st>>>(kp);
     return hipGetLastError();
 }
 

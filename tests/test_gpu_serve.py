@@ -58,7 +58,7 @@ def _run_tables(cached, new, free_list, free_count, table, T, page, alias=False)
 
 
 @pytest.mark.parametrize("B,T,page,new,spare", [(1, 1, 16, 1, 5), (1, 0, 16, 1, 5), (3, 7, 16, 3, 0), (64, 64, 16, 1, 3), (65, 70, 32, 1, 100), (200, 300, 16, 4, 20),
-                                                (200, 4096, 48, 60, 500), (1030, 4097, 16, 5, 300), (2500, 9000, 64, 9, 40), (7, 20000, 16, 5000, 1000), (5, 30000, 1024, 9000, 4)])
+                                                (200, 4096, 48, 60, 500), (1030, 4097, 16, 5, 300), (2500, 9000, 64, 9, 40), (4097, 3000, 16, 2, 900), (6000, 20000, 32, 6, 7000), (7, 20000, 16, 5000, 1000), (5, 30000, 1024, 9000, 4)])
 def test_page_tables(B, T, page, new, spare):
     rng = np.random.default_rng(B * 7 + T)
     max_blocks = 3 + 4 * new // page

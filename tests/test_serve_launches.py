@@ -44,11 +44,21 @@ def _desc(**kw):
     return serve.Desc(**{**dict(B=4, T=4, H=32, S=8, d_pool=128, d_sel=128, page=16, n_blocks=5000, max_blocks=4096), **kw})
 
 
-@pytest.mark.parametrize("T,B,launches", [(1, 1, 1), (256, 64, 1), (257, 64, 1), (4096, 2000, 1), (4097, 10, 2)])
-def test_tables(T, B, launches):
-    run = _run("lca_page_tables", _desc(T=T, B=B, H=1, S=1), [1] * 11)
-    assert len(run) == launches and run[0].grid == 1
-    assert run[0].block == (64 if launches == 1 and B <= 64 and T <= 256 else 1024)
+@pytest.mark.parametrize("T,B,apart,grids", [(1, 1, 0, [1]), (256, 64, 1, [1]), (257, 64, 1, [1]), (4096, 2000, 0, [1]), (4096, 2000, 1, [4]), (4097, 10, 0, [1, 17]),
+                                             (4097, 10, 1, [5]), (131072, 4096, 1, [128]), (131072, 4097, 1, [1, 512]), (0, 5000, 0, [1]), (0, 3, 0, [1])])
+def test_tables(T, B, apart, grids):
+    """One launch, every workgroup with all requests' sums; two where the stack's count is written in place and several would read it, or LDS holds no more requests."""
+    lib = t._load()
+    for n in serve.EXPORTS:
+        getattr(lib, n).argtypes = getattr(serve.load(), n).argtypes
+    lib.trace_reset()
+    d = _desc(T=T, B=B, H=1, S=1)
+    args = [A] * 11
+    args[4] = A + 64 * apart
+    assert lib.lca_page_tables(ctypes.byref(serve._c_desc(*d._key())), *args, A, 1 << 40, None) == lca.OK
+    run = [line.split("\t") for line in lib.trace_log().decode().splitlines()]
+    assert [int(r[1]) for r in run] == grids
+    assert int(run[0][2]) == (64 if B <= 64 and T <= 256 else 1024)
 
 
 @pytest.mark.parametrize("max_q,T,window", [(1, 32, 1), (8, 100, 1), (9, 1000, 16), (0, 8, 1), (0, 1000, 16)])
