@@ -628,42 +628,70 @@ __global__ __launch_bounds__(64 * wavefronts(PAGED, DV), DV <= 128 ? 2 : 1) void
     }
 }
 
-// Joins the parts of every column of the items that have more than one: one wavefront per column.
+// Joins the parts of every column of the items that have more than one: sixteen lanes a column, DV / 16 outputs each.
 template <typename E, int DV, bool PAGED>
 __global__ __launch_bounds__(256) void scored_merge_kernel(const TileParams kp)
 {
     typedef typename Store<E>::type T;
-    constexpr int V = DV / 64, BM = 32 * wavefronts(PAGED, DV);
+    constexpr int N = DV / 16, BM = 32 * wavefronts(PAGED, DV);
     const ServeDims &d = kp.d;
-    const int lane = threadIdx.x & 63, u = blockIdx.x / (BM / 4);
-    const int k = (blockIdx.x % (BM / 4)) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, l16 = lane & 15, u = blockIdx.x / (BM / 16);
+    const int k = (blockIdx.x % (BM / 16)) * 16 + (threadIdx.x >> 4);
     const int y = d.by_S(u), x = kp.items - 1 - y, s = u - y * d.S;
     int item0;
     const int b = request_of_item<BM>(kp.q_start, d, x, lane, item0);
     const Request r = make_request(kp.q_start, kp.seq_len, kp.prefix_len, b, d.T, d.max_blocks * d.page);
-    const int columns = r.rows * d.hps, c_first = (x - item0) * BM, c = c_first + k;
-    if (x < item0 || c >= columns || columns < kp.least) return;
+    const int columns = r.rows * d.hps, c_first = (x - item0) * BM;
+    if (x < item0 || c_first >= columns || columns < kp.least) return;
     const Tiles tiles = make_tiles<BM>(d, kp.rule, r, c_first, columns);
     const int per = max(kp.per_part, kp.by_parts(tiles.count + kp.parts - 1));
     if (tiles.count <= per) return;               // one part: it has written the output
-    const int parts = (tiles.count + per - 1) / per;
+    const int parts = (tiles.count + per - 1) / per, c = c_first + k;
     const float *src = kp.part + ((size_t)u * kp.parts * BM + k) * (DV + 2);
-    float m, l, sum[V];
-    merge_parts<V>(src, (size_t)BM * (DV + 2), parts, lane, m, l, sum);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int row = d.by_hps(c), head = s * d.hps + (c - row * d.hps);
-    const size_t at = (size_t)(r.first + row) * d.H + head;
-    bool fine = true;
-    T o[V];
+    constexpr size_t STEP = (size_t)BM * (DV + 2);
+    float m = -INFINITY, l = 0.f, sum[N];
+    for (int p = l16; p < parts; p += 16) m = fmaxf(m, src[p * STEP]);
+    m = lanes::over_group<16>(m, lanes::Max());
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const float y = sum[v] * inv;
-        fine = fine && fabsf(y) < INFINITY;
-        o[v] = from_float<T>(y);
+    for (int v = 0; v < N; ++v) sum[v] = 0.f;
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) {
+        const float *part = src + p * STEP;
+        const float2 ml = *reinterpret_cast<const float2 *>(part);
+        const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+        l = fmaf(ml.y, f, l);
+#pragma unroll
+        for (int v = 0; v < N; v += 2) {
+            const float2 w = *reinterpret_cast<const float2 *>(part + 2 + l16 * N + v);
+            sum[v] = fmaf(w.x, f, sum[v]);
+            sum[v + 1] = fmaf(w.y, f, sum[v + 1]);
+        }
     }
-    if (lane * V < d.d_pool) __builtin_memcpy(__builtin_assume_aligned((T *)kp.O + at * d.d_pool + lane * V, V * sizeof(T)), o, V * sizeof(T));     // (V divides 8)
-    if (kp.lse != nullptr && lane == 0) kp.lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!fine) != 0, 0)) row_again<E, DV, PAGED>(kp, r, b, s, c, lane);
+    bool fine = true;
+    if (c < columns) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const int row = d.by_hps(c), head = s * d.hps + (c - row * d.hps);
+        const size_t at = (size_t)(r.first + row) * d.H + head;
+        T o[N];
+#pragma unroll
+        for (int v = 0; v < N; ++v) {
+            const float w = sum[v] * inv;
+            fine = fine && fabsf(w) < INFINITY;
+            o[v] = from_float<T>(w);
+        }
+        T *O = (T *)kp.O + at * d.d_pool + l16 * N;
+        // (widths are multiples of 8: pieces of 4 or 8 outputs lie inside or outside; of 16, half of one may)
+#pragma unroll
+        for (int v = 0; v < N; v += 8)
+            if (l16 * N + v < d.d_pool) __builtin_memcpy(__builtin_assume_aligned(O + v, (N < 8 ? N : 8) * sizeof(T)), o + v, (N < 8 ? N : 8) * sizeof(T));
+        if (kp.lse != nullptr && l16 == 0) kp.lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    }
+    unsigned long long odd = __builtin_amdgcn_ballot_w64(!fine);
+    while (__builtin_expect(odd != 0, 0)) {
+        const int g = __builtin_ctzll(odd) >> 4;
+        row_again<E, DV, PAGED>(kp, r, b, s, __builtin_amdgcn_readlane(c, 16 * g), lane);
+        odd &= ~(0xFFFFull << (16 * g));
+    }
 }
 
 // The widths kernels are built for: 64 / 64, 128 / 128, 192 / 128, 256 / 256.
@@ -698,7 +726,7 @@ template <typename E, int DK, int DV, bool PAGED> void run(const TileParams &kp,
     else if (cap) scored_tile_kernel<E, DK, DV, PAGED, true, false><<<grid, 64 * NW, bytes, st>>>(kp);
     else if (bias) scored_tile_kernel<E, DK, DV, PAGED, false, true><<<grid, 64 * NW, bytes, st>>>(kp);
     else scored_tile_kernel<E, DK, DV, PAGED, false, false><<<grid, 64 * NW, bytes, st>>>(kp);
-    if (kp.parts > 1) scored_merge_kernel<E, DV, PAGED><<<(unsigned)((long)kp.items * kp.d.S * (BM / 4)), 256, 0, st>>>(kp);
+    if (kp.parts > 1) scored_merge_kernel<E, DV, PAGED><<<(unsigned)((long)kp.items * kp.d.S * (BM / 16)), 256, 0, st>>>(kp);
 }
 
 template <typename E, bool PAGED> void run_widths(const TileParams &kp, hipStream_t st)
