@@ -145,13 +145,14 @@ PROFILES = {"cfg4": "lca_prefill_cfg4_128k.md", "cfg5": "lca_prefill_cfg5_gqa_64
 
 
 def kernel_sources_sha256() -> str:
-    """Hash of the HIP sources the library is built from (file names and contents, sorted): the stamp a profile
-    summary carries, so that a summary made from other kernels than the tree's is recognised."""
+    """Hash of the HIP sources of the kernels that this program's calls launch (file names and contents, sorted; not the entry points'
+    host code, nor the serving operators, which it does not call): the stamp a profile summary carries, so that a summary made
+    from other kernels than the tree's is recognised."""
     import hashlib
     csrc = os.path.join(os.path.dirname(os.path.abspath(__file__)), "paper_2604_12452_amd", "csrc")
     h = hashlib.sha256()
     for name in sorted(os.listdir(csrc)):
-        if name.endswith((".hip", ".h")):
+        if name.endswith((".hip", ".h")) and not name.startswith(("lca_api", "api_checks", "serve_", "scored_", "page_")):
             h.update(name.encode() + b"\0" + open(os.path.join(csrc, name), "rb").read() + b"\0")
     return h.hexdigest()[:16]
 
