@@ -5,6 +5,7 @@ streams, every step runs in the library's HIP kernels.
 from __future__ import annotations
 
 import ctypes
+import warnings
 from dataclasses import dataclass
 from functools import lru_cache
 from operator import index
@@ -69,11 +70,20 @@ def load() -> ctypes.CDLL:
             f.restype, f.argtypes = ctypes.c_int, args
         _lib = lib
         if lca._bind is not None:
-            import torch
-            lca._bind.setup_serve(Desc, {name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in EXPORTS},
-                                   getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device))
-            _bind = lca._bind
+            _load_bind(lib, lca._bind)
     return _lib
+
+
+def _load_bind(lib, bind) -> None:
+    """The native marshalling of these calls, where lca has it; everything works without it."""
+    global _bind
+    try:
+        import torch
+        bind.setup_serve(Desc, {name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in EXPORTS},
+                         getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device))
+        _bind = bind
+    except Exception as e:
+        warnings.warn(f"{lca.BIND_PATH} is not used by serve, its calls are marshalled in Python: {e}", RuntimeWarning)
 
 
 def workspace_size(desc: Desc) -> int:
@@ -144,7 +154,8 @@ def page_tables(desc: Desc, cached_len, new_len, free_list, free_count, free_lef
     _fit(desc, "i32", (cached_len, "cached_len", B), (new_len, "new_len", B), (free_list, "free_list", desc.n_blocks), (free_count, "free_count", 1),
          (free_left, "free_left", 1), (block_table, "block_table", B * desc.max_blocks), (q_start, "q_start", B + 1), (seq_len, "seq_len", B), (slot, "slot", T),
          (position, "position", T), (request, "request", T))
-    _same_device(cached_len=cached_len, block_table=block_table, slot=slot)
+    _same_device(cached_len=cached_len, new_len=new_len, free_list=free_list, free_count=free_count, free_left=free_left, block_table=block_table, q_start=q_start,
+                 seq_len=seq_len, slot=slot, position=position, request=request, workspace=workspace)
     _call("lca_page_tables", desc, *map(lca._ptr, (cached_len, new_len, free_list, free_count, free_left, block_table, q_start, seq_len, slot, position, request,
                                                    workspace)), lca._nbytes(workspace), lca._stream(stream))
 
@@ -154,7 +165,7 @@ def page_release(desc: Desc, finished, cached_len, block_table, free_list, free_
         return
     _fit(desc, "i32", (finished, "finished", desc.B), (cached_len, "cached_len", desc.B), (block_table, "block_table", desc.B * desc.max_blocks),
          (free_list, "free_list", desc.n_blocks), (free_count, "free_count", 1))
-    _same_device(cached_len=cached_len, block_table=block_table)
+    _same_device(finished=finished, cached_len=cached_len, block_table=block_table, free_list=free_list, free_count=free_count)
     _call("lca_page_release", desc, *map(lca._ptr, (finished, cached_len, block_table, free_list, free_count)), lca._stream(stream))
 
 
@@ -171,7 +182,7 @@ def page_store_q8(desc: Desc, SEL, POOL, slot, sel_q8, pool_q8, scales, stream=N
     _fit_rows(desc, POOL, "POOL", desc.S, desc.d_pool, desc.pool_row)
     _fit(desc, "i32", (slot, "slot", desc.T))
     _fit_cache(desc, sel_q8, pool_q8, scales)
-    _same_device(SEL=SEL, POOL=POOL, slot=slot, sel_q8=sel_q8)
+    _same_device(SEL=SEL, POOL=POOL, slot=slot, sel_q8=sel_q8, pool_q8=pool_q8, scales=scales)
     _call("lca_page_store_q8", desc, _row_ptr(SEL), _row_ptr(POOL), *map(lca._ptr, (slot, sel_q8, pool_q8, scales)), lca._stream(stream))
 
 
@@ -188,7 +199,8 @@ def page_attn_q8(desc: Desc, q, q_start, seq_len, prefix_len, slopes, block_tabl
     _fit(desc, "i32", (q_start, "q_start", desc.B + 1), (seq_len, "seq_len", desc.B), (block_table, "block_table", desc.B * desc.max_blocks))
     _fit_rule(desc, prefix_len, slopes, O, lse)
     _fit_cache(desc, sel_q8, pool_q8, scales)
-    _same_device(q=q, block_table=block_table, sel_q8=sel_q8, O=O)
+    _same_device(q=q, q_start=q_start, seq_len=seq_len, prefix_len=prefix_len, slopes=slopes, block_table=block_table, sel_q8=sel_q8, pool_q8=pool_q8, scales=scales,
+                 O=O, lse=lse, workspace=workspace)
     _call("lca_page_attn_q8", desc, _row_ptr(q), *map(lca._ptr, (q_start, seq_len, prefix_len, slopes, block_table, sel_q8, pool_q8, scales, O, lse, workspace)),
           lca._nbytes(workspace), lca._stream(stream))
 
@@ -201,6 +213,6 @@ def packed_attn(desc: Desc, Q, SEL, POOL, doc_start, prefix_len, slopes, O, lse,
     _fit_rows(desc, POOL, "POOL", desc.S, desc.d_pool, desc.pool_row)
     _fit(desc, "i32", (doc_start, "doc_start", desc.B + 1))
     _fit_rule(desc, prefix_len, slopes, O, lse)
-    _same_device(Q=Q, SEL=SEL, POOL=POOL, O=O)
+    _same_device(Q=Q, SEL=SEL, POOL=POOL, doc_start=doc_start, prefix_len=prefix_len, slopes=slopes, O=O, lse=lse, workspace=workspace)
     _call("lca_packed_attn", desc, _row_ptr(Q), _row_ptr(SEL), _row_ptr(POOL), *map(lca._ptr, (doc_start, prefix_len, slopes, O, lse, workspace)), lca._nbytes(workspace),
           lca._stream(stream))

@@ -152,6 +152,33 @@ def test_a_tensor_on_another_device_is_refused(monkeypatch):
     serve._same_device(K=_Elsewhere())
 
 
+def test_every_tensor_of_a_call_is_held_to_the_current_device(lib, monkeypatch):
+    """Each argument in turn on another device, the others as addresses."""
+    import torch
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(serve, "_bind", None)
+    for name in ("_fit", "_fit_rows", "_fit_cache", "_fit_rule"):
+        monkeypatch.setattr(serve, name, lambda *a: None)
+    d = _desc()
+    for call, n in ((serve.page_tables, 12), (serve.page_release, 5), (serve.page_store_q8, 6), (serve.page_attn_q8, 12), (serve.packed_attn, 9)):
+        for i in range(n):
+            args = [A] * n
+            args[i] = _Elsewhere()
+            with pytest.raises(ValueError, match="is on cuda:1, the current device is cuda:0"):
+                call(d, *args)
+
+
+def test_without_the_native_marshalling(lib, monkeypatch):
+    """A module that does not know these calls, or does not fit, is left alone with a warning."""
+    monkeypatch.setattr(serve, "_bind", None)
+
+    class Older:
+        pass
+    with pytest.warns(RuntimeWarning, match="marshalled in Python"):
+        serve._load_bind(serve.load(), Older)
+    assert serve._bind is None
+
+
 def test_strided_tensors_are_held_to_the_descriptor():
     import torch
     d = _desc(sel_row=160)
