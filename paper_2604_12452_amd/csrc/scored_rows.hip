@@ -1,4 +1,5 @@
-// The scored attention (include/lca_serve.h) row by row, one wavefront per (row, query head): any width and type.
+// The scored attention of packed prompts (include/lca_serve.h) row by row, one wavefront per (row, query head): fp32, widths above 256, tokens
+// farther apart than a buffer descriptor reaches.
 #include "serve_row.h"
 
 namespace lca {
@@ -8,15 +9,13 @@ struct RowsParams {
     const void *Q, *SEL, *POOL;
     void *O;
     float *lse;
-    const int32_t *q_start, *seq_len, *prefix_len, *block_table;
+    const int32_t *q_start, *prefix_len;
     const float *slopes;
-    const uint8_t *sel_q8, *pool_q8;
-    const float *scales;
     ServeDims d;
     ScoreRule rule;
 };
 
-template <typename T, int NV, bool PAGED>
+template <typename T, int NV>
 __global__ __launch_bounds__(256) void scored_rows_kernel(const RowsParams kp)
 {
     const ServeDims &d = kp.d;
@@ -26,44 +25,33 @@ __global__ __launch_bounds__(256) void scored_rows_kernel(const RowsParams kp)
     if (t >= d.T) return;
     const int b = request_of(kp.q_start, d.B, t);
     if (b < 0) return;
-    const Request r = make_request(kp.q_start, kp.seq_len, kp.prefix_len, b, d.T, d.max_blocks * d.page);
+    const Request r = make_request(kp.q_start, nullptr, kp.prefix_len, b, d.T, 0);
     if (t < r.first || t >= r.first + r.rows) return;
     const int i = r.pos0 + t - r.first;
     const float slope = kp.slopes != nullptr ? kp.slopes[h] * LOG2E : 0.f;
     const T *q = (const T *)kp.Q + (size_t)t * d.q_row + (size_t)h * d.d_sel;
     T *O = (T *)kp.O + ((size_t)t * d.H + h) * d.d_pool;
     float *lse = kp.lse != nullptr ? kp.lse + (size_t)t * d.H + h : nullptr;
-    if constexpr (PAGED) {
-        const PagedSource<T> src{kp.block_table + (size_t)b * d.max_blocks, kp.sel_q8, kp.pool_q8, kp.scales, d.page, d.n_blocks, d.S, s, d.d_sel, d.d_pool, d.by_page};
-        scored_row<T, NV>(src, q, r, i, slope, kp.rule, d.d_sel, d.d_pool, O, lse, lane);
-    } else {
-        const PackedSource<T> src{(const T *)kp.SEL + (size_t)r.first * d.sel_row + (size_t)s * d.d_sel,
-                                  (const T *)kp.POOL + (size_t)r.first * d.pool_row + (size_t)s * d.d_pool, d.sel_row, d.pool_row};
-        scored_row<T, NV>(src, q, r, i, slope, kp.rule, d.d_sel, d.d_pool, O, lse, lane);
-    }
+    const PackedSource<T> src{(const T *)kp.SEL + (size_t)r.first * d.sel_row + (size_t)s * d.d_sel,
+                              (const T *)kp.POOL + (size_t)r.first * d.pool_row + (size_t)s * d.d_pool, d.sel_row, d.pool_row};
+    scored_row<T, NV>(src, q, r, i, slope, kp.rule, d.d_sel, d.d_pool, O, lse, lane);
 }
 
-template <typename T, bool PAGED> void run_rows(const RowsParams &kp, hipStream_t st)
+template <typename T> void run_rows(const RowsParams &kp, hipStream_t st)
 {
     const unsigned grid = (unsigned)(((long)kp.d.T * kp.d.H + 3) / 4);
-    if (kp.d.d_pool <= 256) scored_rows_kernel<T, 4, PAGED><<<grid, 256, 0, st>>>(kp);
-    else if constexpr (!PAGED) scored_rows_kernel<T, 16, PAGED><<<grid, 256, 0, st>>>(kp);
+    if (kp.d.d_pool <= 256) scored_rows_kernel<T, 4><<<grid, 256, 0, st>>>(kp);
+    else scored_rows_kernel<T, 16><<<grid, 256, 0, st>>>(kp);
 }
 
 }  // namespace
 
 hipError_t launch_scored_rows(const ScoredArgs &a, hipStream_t st)
 {
-    const RowsParams kp{a.Q, a.SEL, a.POOL, a.O, a.lse, a.q_start, a.seq_len, a.prefix_len, a.block_table, a.slopes, a.sel_q8, a.pool_q8, a.scales, a.d,
-                        score_rule(a.d)};
-    if (a.block_table != nullptr) {
-        if (a.d.dtype == LCA_F16) run_rows<f16_t, true>(kp, st);
-        else run_rows<uint16_t, true>(kp, st);
-    } else {
-        if (a.d.dtype == LCA_F32) run_rows<float, false>(kp, st);
-        else if (a.d.dtype == LCA_F16) run_rows<f16_t, false>(kp, st);
-        else run_rows<uint16_t, false>(kp, st);
-    }
+    const RowsParams kp{a.Q, a.SEL, a.POOL, a.O, a.lse, a.q_start, a.prefix_len, a.slopes, a.d, score_rule(a.d)};
+    if (a.d.dtype == LCA_F32) run_rows<float>(kp, st);
+    else if (a.d.dtype == LCA_F16) run_rows<f16_t>(kp, st);
+    else run_rows<uint16_t>(kp, st);
     return hipGetLastError();
 }
 
