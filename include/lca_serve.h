@@ -48,7 +48,7 @@ typedef struct {
     int32_t max_q, max_kv;      /* most new rows of a request, longest request: hints for how the work is split, 0 = not known; results never depend on
                                    their being right beyond rounding, speed does                                    */
     int32_t window;             /* 0 = none                                                                         */
-    float scale, softcap;       /* softcap 0 = none                                                                 */
+    float scale, softcap;       /* softcap 0 = none; 16-bit types: up to 1024.  Refused where scale * log2(e), 2 softcap * log2(e) or their quotient is beyond fp32 */
     int64_t q_row, sel_row, pool_row;   /* elements between tokens of Q, SEL, POOL (a piece of a fused projection), multiples of 16 bytes; 0 = H * d_sel,
                                    S * d_sel, S * d_pool.  Heads of a token are contiguous; O is always [T,H,d_pool]  */
 } lca_serve_desc;

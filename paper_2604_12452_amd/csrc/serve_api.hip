@@ -14,7 +14,7 @@ using lca::fail;
 using lca::FastDiv;
 using lca::ServeDims;
 
-enum { TABLES = 1, CACHE = 2, ATTENTION = 4 };           // what a call reads of the descriptor
+enum { TABLES = 1, CACHE = 2 };           // what a call reads of the descriptor
 
 lca_status make_dims(const lca_serve_desc *desc, int what, ServeDims &d)
 {
@@ -29,6 +29,10 @@ lca_status make_dims(const lca_serve_desc *desc, int what, ServeDims &d)
     if (desc->max_q < 0 || desc->max_kv < 0) return fail(LCA_ERR_INVALID_ARG, "max_q and max_kv must be >= 0");
     if (!std::isfinite(desc->scale)) return fail(LCA_ERR_INVALID_ARG, "scale is not a finite number");
     if (!std::isfinite(desc->softcap) || desc->softcap < 0.f) return fail(LCA_ERR_INVALID_ARG, "softcap must be a finite number >= 0");
+    if (!lca::in_fp32(lca::score_rule(desc->scale, desc->softcap, desc->window)))
+        return fail(LCA_ERR_INVALID_ARG, "scale (%g) and softcap (%g): the scores' factors leave fp32", (double)desc->scale, (double)desc->softcap);
+    if (desc->softcap > lca::LARGEST_CAP && desc->dtype != LCA_F32)
+        return fail(LCA_ERR_UNSUPPORTED, "softcap (%g) above %g is not supported for the 16-bit types", (double)desc->softcap, (double)lca::LARGEST_CAP);
     const int mult = desc->dtype == LCA_F32 ? 4 : 8;
     if (desc->d_pool <= 0 || desc->d_sel <= 0 || desc->d_pool % mult || desc->d_sel % mult)
         return fail(LCA_ERR_INVALID_ARG, "d_pool and d_sel must be positive multiples of %d", mult);
@@ -173,7 +177,7 @@ lca_status lca_page_attn_q8(const lca_serve_desc *desc, const void *q, const int
                             float *lse, void *workspace, size_t workspace_bytes, void *stream)
 {
     ServeDims d;
-    LCA_TRY(make_dims(desc, CACHE | ATTENTION, d));
+    LCA_TRY(make_dims(desc, CACHE, d));
     LCA_TRY(check_ptr(q, "q", d.T > 0));
     LCA_TRY(check_i32(q_start, "q_start"));
     LCA_TRY(check_i32(seq_len, "seq_len"));
@@ -199,7 +203,7 @@ lca_status lca_packed_attn(const lca_serve_desc *desc, const void *Q, const void
                            const int32_t *prefix_len, const float *slopes, void *O, float *lse, void *workspace, size_t workspace_bytes, void *stream)
 {
     ServeDims d;
-    LCA_TRY(make_dims(desc, ATTENTION, d));
+    LCA_TRY(make_dims(desc, 0, d));
     LCA_TRY(check_ptr(Q, "Q", d.T > 0));
     LCA_TRY(check_ptr(SEL, "SEL", d.T > 0));
     LCA_TRY(check_ptr(POOL, "POOL", d.T > 0));

@@ -1,6 +1,8 @@
 // Internal declarations of the serving operators (include/lca_serve.h): validated sizes, arguments, launchers, and the
 // few device functions that their kernels share.
 #pragma once
+#include <cmath>
+
 #include "lanes.h"
 #include "lca_internal.h"
 #include "lca_serve.h"
@@ -88,21 +90,25 @@ hipError_t launch_scored_tile_paged(const ScoredArgs &a, int least, hipStream_t 
 constexpr float LOG2E = 1.4426950408889634f;
 
 // The score rule in base 2: what the kernels need per call.  With a cap, cap * tanh(x) = cap - 2 cap / (1 + e^(2x)): two
-// hardware instructions at a quarter rate, exact to a few 2^-24 of the cap, and its limits are right at infinities.
+// hardware instructions at a quarter rate, exact to a few 2^-24 of the cap, and its limits are right at infinities.  Small against the
+// rounding of 16-bit weights while the cap is at most LARGEST_CAP (2^-12 of a logit); fp32 takes a tanh that is exact to a few 2^-24 of itself.
+constexpr float LARGEST_CAP = 1024.f;
 struct ScoreRule {
     float scale_log2;              // no cap: logit (base 2) = dot * scale_log2
     float pre, cap_log2;           // cap: logit = cap_log2 - 2 cap_log2 / (1 + 2^(dot * pre)); cap_log2 = 0: no cap
     int window;                    // INT_MAX: none
 };
-inline ScoreRule score_rule(const ServeDims &d)
+inline ScoreRule score_rule(float scale, float softcap, int window)
 {
     ScoreRule r;
-    r.scale_log2 = d.scale * LOG2E;
-    r.cap_log2 = d.softcap * LOG2E;
-    r.pre = d.softcap > 0.f ? 2.f * d.scale / d.softcap * LOG2E : 0.f;
-    r.window = d.window > 0 ? d.window : 0x7FFFFFFF;
+    r.scale_log2 = scale * LOG2E;
+    r.cap_log2 = softcap * LOG2E;
+    r.pre = softcap > 0.f ? 2.f * scale / softcap * LOG2E : 0.f;
+    r.window = window > 0 ? window : 0x7FFFFFFF;
     return r;
 }
+inline ScoreRule score_rule(const ServeDims &d) { return score_rule(d.scale, d.softcap, d.window); }
+inline bool in_fp32(const ScoreRule &r) { return std::isfinite(r.scale_log2) && std::isfinite(2.f * r.cap_log2) && std::isfinite(r.pre); }
 template <bool CAP> __device__ __forceinline__ float capped(float dot, const ScoreRule &r)
 {
     if constexpr (!CAP) return dot * r.scale_log2;

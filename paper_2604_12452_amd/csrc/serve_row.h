@@ -127,7 +127,8 @@ __device__ __forceinline__ void scored_row(const Source &src, const T *q, const 
         float s = -INFINITY;
         if (x < count && src.has(j)) {
             const float dot = src.dot(q, j, d_sel);
-            s = rule.cap_log2 > 0.f ? capped<true>(dot, rule) : capped<false>(dot, rule);
+            if constexpr (sizeof(T) == 4) s = rule.cap_log2 > 0.f ? rule.cap_log2 * tanhf(dot * rule.pre * (0.5f / LOG2E)) : capped<false>(dot, rule);
+            else s = rule.cap_log2 > 0.f ? capped<true>(dot, rule) : capped<false>(dot, rule);
             s = fmaf(-slope, fabsf((float)(i - j)), s);
         }
         const float top = fmaxf(m, lanes::over_group<64>(s, lanes::Max()));

@@ -318,6 +318,25 @@ def test_packed_large_logits(dtype):
     _check_packed(Q, SEL, POOL, [0, T], dtype, 2.0, dict(softcap=200.0, window=100))
 
 
+@pytest.mark.parametrize("softcap", [1024.0, 1e6])
+def test_packed_fp32_caps_far_above_the_scores(softcap):
+    """The cap bends scores of a few units by next to nothing and must not cost them its own 2^-24: the bound is that of no cap (its slope is at most one),
+    and 2^-20 of the logits for the hyperbolic tangent, its argument and the change of base."""
+    rng = np.random.default_rng(8)
+    Q, SEL, POOL = (_randn(rng, "f32", 90, 2, 64) for _ in range(3))
+    torch, lca, serve = _api()
+    d = serve.Desc(B=1, T=90, H=2, S=2, d_pool=64, d_sel=64, dtype=lca.F32, scale=0.5, softcap=softcap)
+    O, lse = torch.empty_like(Q), torch.empty(90, 2, device="cuda")
+    serve.packed_attn(d, Q, SEL, POOL, _i32([0, 90]), None, None, O, lse, serve.alloc_workspace(d))
+    for h in range(2):
+        q, k, v = _f64(Q)[:, h], _f64(SEL)[:, h], _f64(POOL)[:, h]
+        want = ref.attend(q, k, v, np.arange(90), 90, "f32", scale=0.5, softcap=softcap)
+        bound = ref.attend(q, k, v, np.arange(90), 90, "f32", scale=0.5)
+        logit = 2.0 ** -20 * 0.5 * np.abs(q @ k.T).max()
+        _close(_f64(O)[:, h], want[0], bound[2] + 2 * logit * np.abs(v).max(), (h, "O"))
+        _close(_f64(lse)[:, h], want[1], bound[3] + logit, (h, "lse"))
+
+
 def test_packed_pieces_of_a_fused_projection():
     rng = np.random.default_rng(11)
     T, H, S, d = 130, 6, 2, 64

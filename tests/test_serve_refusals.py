@@ -49,7 +49,8 @@ def _desc(**kw):
 
 
 ANY = [dict(B=0), dict(B=-1), dict(T=-1), dict(H=0), dict(S=0), dict(S=3), dict(dtype=3), dict(dtype=-1), dict(d_pool=0), dict(d_sel=12), dict(d_pool=1032), dict(window=-1),
-       dict(scale=float("nan")), dict(scale=float("inf")), dict(softcap=float("nan")), dict(softcap=-1.0), dict(softcap=float("inf")), dict(max_q=-1), dict(max_kv=-2),
+       dict(scale=float("nan")), dict(scale=float("inf")), dict(softcap=float("nan")), dict(softcap=-1.0), dict(softcap=float("inf")), dict(softcap=1e-40), dict(softcap=3e38, dtype=lca.F32), dict(scale=3e38), dict(softcap=1025.0),
+       dict(softcap=1025.0, dtype=lca.F16), dict(max_q=-1), dict(max_kv=-2),
        dict(T=1 << 28, H=8), dict(B=1 << 24), dict(q_row=8), dict(q_row=8 * 64 + 4), dict(sel_row=120), dict(pool_row=-128), dict(pool_row=1 << 33)]
 PAGES = [dict(page=0), dict(page=8), dict(page=24), dict(page=2048), dict(n_blocks=0), dict(n_blocks=1 << 27), dict(max_blocks=0), dict(max_blocks=(1 << 26) + 1)]
 CACHE = [dict(dtype=lca.F32), dict(d_pool=72), dict(d_sel=264), dict(d_sel=512)]
@@ -97,6 +98,11 @@ def test_a_workspace_that_is_missing_or_too_small(lib):
     assert lib.lca_page_tables(cd, *[A] * 11, 0, need, 0) == lca.ERR_WORKSPACE
     assert lib.lca_page_tables(cd, *[A] * 11, A + 4, need, 0) == lca.ERR_INVALID_ARG
     assert lib.lca_page_tables(cd, *[A] * 11, A, 3999, 0) == lca.ERR_WORKSPACE and b"needed" in lib.lca_last_error()
+
+
+def test_the_largest_caps_are_taken(lib):
+    for kw in (dict(softcap=1024.0), dict(softcap=1024.0, dtype=lca.F16), dict(softcap=1e30, dtype=lca.F32)):
+        assert serve.workspace_size(_desc(**kw)) > 0
 
 
 def test_no_rows_is_no_call(lib):
