@@ -114,14 +114,14 @@ struct Call {
 
 enum Kind { ELT, I32, F32, U8, ANY };
 
-// Address of a tensor of at least `elems` elements of the kind asked for; false if lca.py has to look at it.
-bool address(PyObject *o, int32_t dtype, Kind kind, int64_t elems, bool optional, void *&out)
+// Address of a tensor of at least `elems` elements of the kind asked for; false if lca.py has to look at it.  strided: its caller has seen the strides.
+bool address(PyObject *o, int32_t dtype, Kind kind, int64_t elems, bool optional, void *&out, bool strided = false)
 {
     out = nullptr;
     if (o == Py_None) return optional || elems == 0;
     if (!THPVariable_CheckExact(o)) return false;
     const at::Tensor &t = THPVariable_Unpack(o);
-    if (!t.defined() || !t.is_cuda() || !t.has_storage() || !t.is_contiguous()) return false;
+    if (!t.defined() || !t.is_cuda() || !t.has_storage() || (!strided && !t.is_contiguous())) return false;
     const at::ScalarType s = t.scalar_type();
     switch (kind) {
     case ELT:
@@ -377,10 +377,10 @@ struct ServeArgs {
         ok = ok && d.B > 0 && d.T >= 0 && d.H > 0 && d.S > 0 && d.d_pool > 0 && d.d_sel > 0 && d.page >= 0 && d.n_blocks >= 0 && d.max_blocks >= 0;
         ok = ok && (d.dtype == LCA_BF16 || d.dtype == LCA_F32 || d.dtype == LCA_F16);
     }
-    void *take(Kind kind, Count elems, bool optional = false)
+    void *take(Kind kind, Count elems, bool optional = false, bool strided = false)
     {
         void *p = nullptr;
-        if (ok) ok = address(*o, d.dtype, kind, elems.v, optional, p);
+        if (ok) ok = address(*o, d.dtype, kind, elems.v, optional, p, strided);
         if (ok && *o != Py_None) {               // all on one device
             const int64_t here = THPVariable_Unpack(*o).get_device();
             ok = device < 0 || device == here;
@@ -392,6 +392,12 @@ struct ServeArgs {
     void *rows(int64_t heads, int64_t width, int64_t row)      // [T, heads, width], tokens `row` elements apart
     {
         const Count one = Count{heads} * width, before = Count{d.T - 1} * (row != 0 ? row : one.v);
+        if (ok && THPVariable_CheckExact(*o)) {                // a piece of a wider tensor, as serve.py's _fit_rows has it
+            const at::Tensor &t = THPVariable_Unpack(*o);
+            if (t.defined() && t.dim() == 3 && !t.is_contiguous() && t.size(0) == d.T && t.size(1) == heads && t.size(2) == width && t.stride(2) == 1 &&
+                (heads == 1 || t.stride(1) == width) && (d.T <= 1 || t.stride(0) == (row != 0 ? row : one.v)))
+                return take(ELT, Count{0}, false, true);
+        }
         int64_t elems = 0;
         if (d.T > 0 && __builtin_add_overflow(before.v, one.v, &elems)) elems = INT64_MAX;
         return take(ELT, Count{elems});

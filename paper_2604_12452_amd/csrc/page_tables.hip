@@ -24,14 +24,15 @@ struct TablesParams {
 
 constexpr int REFUSED = -1;                       // base of a request that gets nothing
 
-// Inclusive prefix sum over the workgroup, saturating at `limit` (values >= 0, each <= limit, limit < 2^30).
+// Inclusive prefix sum over the workgroup, saturating at `limit` (values >= 0, each <= limit, limit <= 2^30: two of them fit 32 bits without a sign).
+__device__ __forceinline__ int add_up_to(int a, int b, int limit) { return (int)min((unsigned)a + (unsigned)b, (unsigned)limit); }
 template <int WAVES> __device__ __forceinline__ int scan_up_to(int v, int limit, int *lds, int tid)
 {
     const int lane = tid & 63, wave = tid >> 6;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
         const int w = __shfl_up(v, o, 64);
-        if (lane >= o) v = min(v + w, limit);
+        if (lane >= o) v = add_up_to(v, w, limit);
     }
     if constexpr (WAVES == 1) return v;
     if (lane == 63) lds[wave] = v;
@@ -39,9 +40,9 @@ template <int WAVES> __device__ __forceinline__ int scan_up_to(int v, int limit,
     int before = 0;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w)
-        if (w < wave) before = min(before + lds[w], limit);
+        if (w < wave) before = add_up_to(before, lds[w], limit);
     __syncthreads();
-    return min(v + before, limit);
+    return add_up_to(v, before, limit);
 }
 
 // A token's slot and request: t < T, b its request (its first row, its base) or -1.
@@ -82,12 +83,12 @@ template <int WAVES, typename Put> __device__ __forceinline__ int take_requests(
         const bool real = b < kp.B;
         const int cached = real ? kp.cached_len[b] : 0, asked = real ? kp.new_len[b] : 0;
         const int add = min(max(asked, 0), T1);
-        const int end = min(scan_up_to<WAVES>(add, T1, lds, tid) + rows, T1);
+        const int end = add_up_to(scan_up_to<WAVES>(add, T1, lds, tid), rows, T1);
         const long total = (long)cached + add;
         const bool fits = real && cached >= 0 && asked >= 0 && end <= kp.T && total <= (long)kp.max_blocks * kp.page;
         const int have = fits ? kp.by_page(cached + kp.page - 1) : 0;
         const int need = fits ? min(kp.by_page((int)total + kp.page - 1) - have, P1) : 0;
-        const int upto = min(scan_up_to<WAVES>(need, P1, lds, tid) + blocks, P1);
+        const int upto = add_up_to(scan_up_to<WAVES>(need, P1, lds, tid), blocks, P1);
         const bool ok = fits && (need == 0 || upto <= free);
         if (real) put(b, min(end, kp.T), ok ? (int)total : 0, ok ? max(free - 1 - (upto - need), 0) : REFUSED);      // (needs none: any base but REFUSED)
         if (ok && need > 0) taken = upto;

@@ -166,7 +166,7 @@ lca_status lca_page_store_q8(const lca_serve_desc *desc, const void *SEL, const 
     LCA_TRY(check_i32(slot, "slot", d.T > 0));
     LCA_TRY(check_ptr(sel_q8, "sel_q8"));
     LCA_TRY(check_ptr(pool_q8, "pool_q8"));
-    LCA_TRY(check_ptr(scales, "scales"));
+    LCA_TRY(check_i32(scales, "scales"));
     if (d.T == 0) return LCA_OK;
     const lca::StoreArgs a{d, SEL, POOL, slot, sel_q8, pool_q8, scales};
     return LCA_LAUNCH(lca::launch_page_store_q8(a, static_cast<hipStream_t>(stream)), "lca_page_store_q8");
@@ -186,7 +186,7 @@ lca_status lca_page_attn_q8(const lca_serve_desc *desc, const void *q, const int
     LCA_TRY(check_i32(block_table, "block_table"));
     LCA_TRY(check_ptr(sel_q8, "sel_q8"));
     LCA_TRY(check_ptr(pool_q8, "pool_q8"));
-    LCA_TRY(check_ptr(scales, "scales"));
+    LCA_TRY(check_i32(scales, "scales"));
     LCA_TRY(check_ptr(O, "O", d.T > 0));
     LCA_TRY(check_i32(lse, "lse", false));
     if (d.T == 0) return LCA_OK;

@@ -90,6 +90,14 @@ def test_pointers_that_are_missing_or_not_aligned(lib, name, pointers, optional)
     assert getattr(lib, name)(None, *[A] * pointers, *rest) == lca.ERR_INVALID_ARG
 
 
+def test_float_arrays_need_four_bytes_of_alignment(lib):
+    """(T = 0 ends behind the checks)"""
+    cd = ctypes.byref(serve._c_desc(*_desc(T=0)._key()))
+    assert lib.lca_page_store_q8(cd, A, A, A, A, A, A + 4, 0) == lca.OK
+    assert lib.lca_page_attn_q8(cd, A, A, A, 0, A + 4, A, A, A, A + 4, A, A + 4, A, 1 << 40, 0) == lca.OK
+    assert lib.lca_packed_attn(cd, A, A, A, A, 0, A + 4, A, A + 4, A, 1 << 40, 0) == lca.OK
+
+
 def test_a_workspace_that_is_missing_or_too_small(lib):
     d = _desc(B=1000, max_q=1)
     need = serve.workspace_size(d)
