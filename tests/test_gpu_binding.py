@@ -107,3 +107,74 @@ def test_what_it_leaves_to_python():
                dict(desc=None), dict(stream="none")):
         assert call(**kw) == -1, kw
     torch.cuda.synchronize()
+
+
+def _serving_step(serve, d, fused, ws):
+    """Every serving call the native marshalling knows, over pieces of one wide tensor, twice: a request's first tokens, then a token each."""
+    import torch
+    B, T, H, S, D = d.B, d.T, d.H, d.S, d.d_sel
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")       # noqa: E731
+    Q, K, V = fused[:, :H * D].unflatten(1, (H, D)), fused[:, H * D:(H + S) * D].unflatten(1, (S, D)), fused[:, (H + S) * D:].unflatten(1, (S, D))
+    sel_q8, pool_q8, scales = serve.alloc_cache(d)
+    cached, free, count, left = i32(0, 0), torch.arange(d.n_blocks, dtype=torch.int32, device="cuda"), i32(d.n_blocks), i32(0)
+    table = torch.full((B, d.max_blocks), -1, dtype=torch.int32, device="cuda")
+    out = []
+    for new in ((7, T - 7), (1, 1)):
+        start, lens, added = i32(0, 0, 0), i32(0, 0), i32(*new)
+        slot, position, request = (torch.zeros(T, dtype=torch.int32, device="cuda") for _ in range(3))
+        O, lse = torch.zeros(T, H, D, dtype=fused.dtype, device="cuda"), torch.zeros(T, H, device="cuda")
+        serve.page_tables(d, cached, added, free, count, left, table, start, lens, slot, position, request, ws)
+        serve.page_store_q8(d, K, V, slot, sel_q8, pool_q8, scales)
+        serve.page_attn_q8(d, Q, start, lens, None, None, table, sel_q8, pool_q8, scales, O, lse, ws)
+        out += [left, table.clone(), start, lens, slot, position, request, O, lse]
+        cached, count = lens, left.clone()
+    O, lse = torch.zeros(T, H, D, dtype=fused.dtype, device="cuda"), torch.zeros(T, H, device="cuda")
+    serve.packed_attn(d, Q, K, V, i32(0, 7, T), None, None, O, lse, ws)
+    serve.page_release(d, i32(1, 0), cached, table, free, count)
+    return out + [O, lse, sel_q8, pool_q8, scales, cached, table, free, count]
+
+
+@pytest.mark.parametrize("dtype", [lca.BF16, lca.F16])
+def test_both_ways_make_the_serving_calls_alike(monkeypatch, dtype):
+    import torch
+
+    from paper_2604_12452_amd import serve
+    serve.load()
+    assert serve._bind is not None, "the native marshalling was not built"
+    row = 8 * 64
+    d = serve.Desc(B=2, T=50, H=4, S=2, d_pool=64, d_sel=64, dtype=dtype, page=16, n_blocks=9, max_blocks=5, scale=0.125, q_row=row, sel_row=row, pool_row=row)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(4)
+    fused = torch.randn(50, row, generator=gen, device="cuda").to(lca.torch_dtype(d))
+    ws = serve.alloc_workspace(d)
+    counted = _Counted(serve._bind)
+    monkeypatch.setattr(serve, "_bind", counted)
+    native = _serving_step(serve, d, fused, ws)
+    assert [s for _, s in counted.seen] == [0] * 8 and len({n for n, _ in counted.seen}) == 5, counted.seen
+    monkeypatch.setattr(serve, "_bind", None)
+    plain = _serving_step(serve, d, fused, ws)
+    torch.cuda.synchronize()
+    for a, b in zip(native, plain):
+        assert torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
+
+
+def test_what_the_serving_calls_leave_to_python():
+    """Tokens that do not lie as the descriptor says, views with gaps between their heads, raw addresses, other classes and types."""
+    import torch
+
+    from paper_2604_12452_amd import serve
+    serve.load()
+    d = serve.Desc(B=1, T=20, H=2, S=1, d_pool=64, d_sel=64, q_row=256)
+    z = lambda *s, dtype=torch.bfloat16: torch.zeros(*s, dtype=dtype, device="cuda")     # noqa: E731
+    wide, K, O, ws, start = z(20, 4, 64), z(20, 1, 64), z(20, 2, 64), serve.alloc_workspace(d), torch.tensor([0, 20], dtype=torch.int32, device="cuda")
+    call = lambda desc=d, Q=wide[:, :2], K=K, O=O, ws=ws, stream=None: serve._bind.packed_attn(desc, Q, K, K, start, None, None, O, None, ws, stream)   # noqa: E731
+    assert call() == 0
+
+    class Other(serve.Desc):
+        pass
+
+    for kw in (dict(Q=wide[:, ::2]), dict(Q=wide[:19, :2]), dict(Q=z(20, 5, 64)[:, :2]), dict(Q=z(20, 2, 128)[:, :, ::2]), dict(Q=wide[:, :2].float()), dict(Q=wide[:, :2].data_ptr()),
+               dict(K=z(20, 2, 64)[:, :1]), dict(O=wide[:, :2]), dict(O=None), dict(ws=None), dict(desc=Other(**d.__dict__)), dict(desc=serve.Desc(**{**d.__dict__, "q_row": 1 << 40})),
+               dict(desc=serve.Desc(**{**d.__dict__, "T": 1 << 40})), dict(desc=None), dict(stream="none")):
+        assert call(**kw) == -1, kw
+    torch.cuda.synchronize()
