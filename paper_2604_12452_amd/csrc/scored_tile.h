@@ -276,15 +276,16 @@ __global__ __launch_bounds__(64 * wavefronts(PAGED, DV), DV <= 128 ? 2 : 1) void
         const int blk = kp.block_table[(size_t)b * d.max_blocks + d.by_strips(min(strip, strip_end - 1))];
         k_block = strip < strip_end && (unsigned)blk < (unsigned)d.n_blocks ? blk : -1;
     };
+    // (a strip's DK or DV threads are whole wavefronts: its block and addresses are a wavefront's)
     auto load_keys = [&](int t) __attribute__((always_inline)) {
         const int strip0 = first_key(t) / 16;
 #pragma unroll
         for (int i = 0; i < K_PIECES; ++i) {
-            const int u = i * THREADS + tid, j = u / (DK / 16), piece = u % (DK / 16), strip = strip0 + (j >> 4);
-            const int blk = __shfl(k_block, j >> 4, 64);
-            const size_t unit = (size_t)max(blk, 0) * d.S + s;
+            const int u = i * THREADS + tid, j = u / (DK / 16) & 15, piece = u % (DK / 16), st = (i * THREADS + 64 * wave) / DK, strip = strip0 + st;
+            const size_t unit = (size_t)max(__builtin_amdgcn_readlane(k_block, st & 3), 0) * d.S + s;
+            const uint8_t *at = kp.sel_q8 + (unit * d.page + (strip - d.by_strips(strip) * strips) * 16) * d.d_sel;
             kreg[i] = make_uint4(0, 0, 0, 0);
-            if (u < K_TOTAL && 16 * piece < d.d_sel) kreg[i] = *reinterpret_cast<const uint4 *>(kp.sel_q8 + (unit * d.page + (strip - d.by_strips(strip) * strips) * 16 + (j & 15)) * d.d_sel + 16 * piece);
+            if (st < 4 && 16 * piece < d.d_sel) kreg[i] = *reinterpret_cast<const uint4 *>(at + (unsigned)(j * d.d_sel + 16 * piece));
             k_scale[i] = kp.scales[2 * unit + 1];
         }
     };
@@ -292,11 +293,12 @@ __global__ __launch_bounds__(64 * wavefronts(PAGED, DV), DV <= 128 ? 2 : 1) void
         const int strip0 = first_key(t) / 16;
 #pragma unroll
         for (int i = 0; i < V_PIECES; ++i) {
-            const int u = i * THREADS + tid, strip = strip0 + u / DV, col = u % DV;
-            const int blk = __shfl(v_block, u / DV, 64);
+            const int u = i * THREADS + tid, col = u % DV, st = (i * THREADS + 64 * wave) / DV, strip = strip0 + st;
+            const int blk = __builtin_amdgcn_readlane(v_block, st & 3);
             const size_t unit = (size_t)max(blk, 0) * d.S + s;
+            const uint8_t *at = kp.pool_q8 + (unit * strips + strip - d.by_strips(strip) * strips) * 16 * d.d_pool;
             vreg[i] = make_uint4(0, 0, 0, 0);
-            if (u < V_TOTAL && col < d.d_pool && blk >= 0) vreg[i] = *reinterpret_cast<const uint4 *>(kp.pool_q8 + ((unit * strips + strip - d.by_strips(strip) * strips) * d.d_pool + col) * 16);
+            if (st < 4 && col < d.d_pool && blk >= 0) vreg[i] = *reinterpret_cast<const uint4 *>(at + (unsigned)(16 * col));
             v_scale[i] = kp.scales[2 * unit];
         }
     };
