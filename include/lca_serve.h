@@ -63,7 +63,8 @@ lca_status lca_serve_workspace_size(const lca_serve_desc *desc, size_t *bytes);
  * in request order: with need_b = ceil((cached_len + new_len) / page) - ceil(cached_len / page) and cum_b its sum up to and
  * including b, the r-th of request b is free_list[free_count - 1 - (cum_b - need_b) - r].
  * A request is refused -- gets no blocks, slots of -1, seq_len 0 -- if its rows end behind T, its tokens do not fit
- * max_blocks, a length is negative (need_b = 0 in these cases), or need_b > 0 and cum_b > free_count.
+ * max_blocks, a length is negative (need_b = 0 in these cases), or need_b > 0 and cum_b > free_count.  What it holds stays as it
+ * is: its cached_len is the caller's to keep (seq_len of the others is their next cached_len).
  * In:  cached_len, new_len [B], free_list [n_blocks], free_count [1].
  * Out: free_left [1] (may be free_count itself), block_table [B,max_blocks] (new entries only), q_start [B+1] (clamped to T),
  *      seq_len [B] (cached_len + new_len), slot, position, request [T] (rows behind the last request: -1, 0, -1).

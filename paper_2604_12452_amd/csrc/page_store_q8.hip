@@ -9,7 +9,8 @@
 // Keys: a lane takes sixteen columns of a token, 32 bytes in, 16 out.  Values lie sixteen tokens of a column next to each other: a lane
 // takes sixteen tokens of a pair of columns, reads them four bytes at a time (a wavefront: 256 bytes of a row) and writes two
 // whole 16-byte pieces; a piece that holds older tokens, or places behind the new ones, is read first and keeps them.
-// Bound by memory: two bytes read and one written per element.
+// Bound by memory: two bytes read and one written per element.  50064 tokens, 8 heads of 128 + 128, blocks of 64: 74 us, 4.16 TB/s (a copy: 4.75).
+// 32 single tokens into blocks of 16: 5.3 to 5.8 us, latency.
 #include "serve_internal.h"
 
 namespace lca {
