@@ -61,8 +61,9 @@ def test_tables(T, B, apart, grids):
     assert int(run[0][2]) == (64 if B <= 64 and T <= 256 else 1024)
 
 
-@pytest.mark.parametrize("max_q,T,window", [(1, 32, 1), (8, 100, 1), (9, 1000, 16), (0, 8, 1), (0, 1000, 16)])
+@pytest.mark.parametrize("max_q,T,window", [(1, 32, 1), (8, 32, 2), (8, 4000, 16), (500, 2000, 16), (0, 8, 1), (0, 1000, 16), (0, 100000, 64)])
 def test_store(max_q, T, window):
+    """A wavefront's window is as long as the runs of tokens (4 requests), less where short ones may fill it."""
     (run,) = _run("lca_page_store_q8", _desc(T=T, max_q=max_q), [1] * 6, ws=False)
     assert run.grid == -(-(-(-T // window)) * 8 * 2 // 4)
 
