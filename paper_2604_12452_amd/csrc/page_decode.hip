@@ -15,7 +15,7 @@
 // a CU to itself); the loads of its next tile are issued as soon as the registers of this one are free.  Softmax with a running maximum, sums in fp32 of the
 // weights before they are rounded.  Parts of long requests are joined by page_merge_kernel.
 // 32 requests of 65536 tokens, 32 heads over 8, 128 / 128: 0.68 to 0.73 ms, 5.9 to 6.3 TB/s, what a plain read reaches (4.31 GB fetched, 4.30 needed).
-// One of 500 tokens, 28 heads over 4: 8.6 us, a chain of launch, starts, table, codes, join.
+// One of 500 tokens, 28 heads over 4: 8.9 us, a chain of launch, starts, table, codes, join.
 #include <algorithm>
 
 #include "serve_row.h"
@@ -63,13 +63,14 @@ struct DecodeParams {
     const float *scales;
     ServeDims d;
     ScoreRule rule;
-    int parts, per_part;                  // workgroups of a (request, KV head, group of columns); least tiles of one
+    int parts;                            // workgroups of a (request, KV head, group of columns)
     int groups;                           // groups of 16 NCT columns
-    FastDiv by_parts, by_groups;
+    FastDiv by_parts, by_groups, by_pairs;
     int most;                             // requests of more columns are left to the chunk kernel (INT_MAX: none)
 };
 
 constexpr int TILE = 64;
+constexpr int LEAST_TILES = 8;            // of a part (24 requests of 4 rows, window 4096, in up to ten parts: 13.7 us, 14.3 with four, 16.9 with sixteen)
 // Whether a wavefront needs the registers of two.
 constexpr bool heavy(int dv, int nct) { return dv * nct >= 256; }
 
@@ -132,9 +133,10 @@ __global__ __launch_bounds__(64 * W, heavy(DV, NCT) ? 1 : 2) void page_decode_ke
     const ServeDims &d = kp.d;
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, q4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int unit = kp.by_parts((int)blockIdx.x), part = blockIdx.x - unit * kp.parts;
-    const int pair = kp.by_groups(unit), group = unit - pair * kp.groups;
-    const int b = d.by_S(pair), s = pair - b * d.S;
+    // first part 0 of all pairs, then part 1: what is split by a hint of long requests and has short ones still falls on every XCD (workgroups go to
+    // them in turn: 32 requests of 4000 tokens with room for 131072, 32 heads over 8, 123 us with a pair's parts next to each other, 51 so)
+    const int outer = kp.by_pairs((int)blockIdx.x), pair = blockIdx.x - outer * (d.B * d.S), part = kp.by_groups(outer), group = outer - part * kp.groups;
+    const int unit = pair * kp.groups + group, b = d.by_S(pair), s = pair - b * d.S;
     const Request r = make_request(kp.q_start, kp.seq_len, kp.prefix_len, b, d.T, d.max_blocks * d.page);
     const int columns = r.rows * d.hps;
     if (columns == 0 || columns > kp.most) return;
@@ -143,7 +145,7 @@ __global__ __launch_bounds__(64 * W, heavy(DV, NCT) ? 1 : 2) void page_decode_ke
     const bool many = columns > kp.groups * 16 * NCT;
     const int parts = many ? 1 : kp.parts;
     if (part >= parts) return;
-    const int per = max(kp.per_part, many ? tiles.count : kp.by_parts(tiles.count + kp.parts - 1));
+    const int per = max(LEAST_TILES, many ? tiles.count : kp.by_parts(tiles.count + kp.parts - 1));
     const int lo = part * per, hi = many ? tiles.count : min(lo + per, tiles.count);
     if (lo >= hi && part > 0) return;                                          // (nothing to see at all: part 0 writes it)
     const bool whole = lo == 0 && hi == tiles.count;                           // this workgroup has the request to itself
@@ -402,7 +404,7 @@ __global__ __launch_bounds__(256) void page_merge_kernel(const DecodeParams kp)
     const int columns = r.rows * d.hps, column = group * columns_per_unit + k;
     if (column >= columns || columns > kp.most || columns > kp.groups * columns_per_unit) return;
     const Tiles tiles = make_tiles(r, kp.rule.window);
-    const int per = max(kp.per_part, kp.by_parts(tiles.count + kp.parts - 1));
+    const int per = max(LEAST_TILES, kp.by_parts(tiles.count + kp.parts - 1));
     if (tiles.count <= per) return;                                            // one part: it has written the output
     const int parts = (tiles.count + per - 1) / per;
     const float *src = kp.part + ((size_t)unit * kp.parts * columns_per_unit + k) * (DV + 2);
@@ -412,7 +414,7 @@ __global__ __launch_bounds__(256) void page_merge_kernel(const DecodeParams kp)
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(!fine) != 0, 0)) row_again<E, DV>(kp, r, b, s, column, lane);
 }
 
-struct Plan { int nct, groups, parts, per_part, waves; };
+struct Plan { int nct, groups, parts, waves; };
 
 // How a call is split, from its sizes and hints.
 Plan make_plan(const ServeDims &d)
@@ -433,12 +435,10 @@ Plan make_plan(const ServeDims &d)
     // four times.  Up to 16 tiles, and up to 64 where there is a workgroup per CU without it, nothing is split and there is nothing to join: 500
     // tokens, 28 heads over 4, 9.9 us, 11.4 in two parts; 64 requests of up to 1500, 17 us, 25 in two.
     const long target = heavy(dv, p.nct) ? 256 : 1024;
-    long parts = tiles <= 16 || (units >= 256 && tiles <= 64) ? 1 : std::max<long>(1, std::min<long>(target / units, (tiles + 3) / 4));
+    p.parts = tiles <= 16 || (units >= 256 && tiles <= 64) ? 1 : (int)std::max<long>(1, std::min<long>(target / units, (tiles + 3) / 4));
     // Eight wavefronts where all of them run at once and nothing is split: 500 tokens 9.1 us with four, 8.6 with eight; where there are more
     // workgroups than CUs (64 requests of up to 1500) 17 and 21, where parts are joined (one request of 2000) 11.2 and 12.2.
-    p.waves = !heavy(dv, p.nct) && parts == 1 && units <= 256 && tiles > 4 ? 8 : 4;
-    p.per_part = (int)((tiles + parts - 1) / parts);
-    p.parts = (int)((tiles + p.per_part - 1) / p.per_part);
+    p.waves = !heavy(dv, p.nct) && p.parts == 1 && units <= 256 && tiles > 4 ? 8 : 4;
     return p;
 }
 
@@ -481,7 +481,7 @@ hipError_t launch_page_decode(const ScoredArgs &a, int most, hipStream_t st)
 {
     const Plan p = make_plan(a.d);
     const DecodeParams kp{a.Q, a.O, a.lse, a.part, a.q_start, a.seq_len, a.prefix_len, a.block_table, a.slopes, a.sel_q8, a.pool_q8, a.scales, a.d, score_rule(a.d),
-                          p.parts, p.per_part, p.groups, FastDiv(p.parts), FastDiv(p.groups), most};
+                          p.parts, p.groups, FastDiv(p.parts), FastDiv(p.groups), FastDiv(a.d.B * a.d.S), most};
     if (a.d.dtype == LCA_F16) run_widths<_Float16>(kp, p, st);
     else run_widths<__bf16>(kp, p, st);
     return hipGetLastError();

@@ -23,7 +23,7 @@
 // Sums are in fp32 of the weights before they are rounded.
 // Bound by the matrix core and the vector ALU, which take turns more than they overlap.  16384 tokens in three documents, 16 heads over 4, 192 / 128:
 // 0.48 ms, 1.11 PFLOP/s (matrix core 59 % of the cycles, vector ALU 43 %; a plain product of 16384^3 reaches 1.33).  8192 tokens, 32 heads over 8, 128 / 128,
-// capped: 0.60 to 0.65 ms, 0.9 PFLOP/s (42 and 67 %).  Over the cache, 700 rows against 9000 tokens and five smaller requests, 32 heads over 8: 175 us, 0.59 PFLOP/s.
+// capped: 0.60 to 0.65 ms, 0.9 PFLOP/s (42 and 67 %).  Over the cache, 700 rows against 9000 tokens and five smaller requests, 32 heads over 8: 167 us, 0.61 PFLOP/s.
 #pragma once
 #include <algorithm>
 #include <type_traits>
@@ -90,8 +90,8 @@ struct TileParams {
     ScoreRule rule;
     int items;                                    // per KV head
     int least;                                    // requests of fewer (row, head) pairs per KV head are another kernel's
-    int parts, per_part;                          // workgroups of an item; least tiles of one
-    FastDiv by_parts;
+    int parts;                                    // workgroups of an item
+    FastDiv by_parts, by_units;                   // items * S
     float *part;                                  // their results, [item, KV head, part, BM, DV + 2]
 };
 
@@ -99,6 +99,7 @@ struct TileParams {
 // the width takes the registers of two wavefronts per SIMD.
 constexpr int wavefronts(bool paged, int dv) { return paged && dv <= 128 ? 8 : 4; }
 constexpr int BN = 64;                            // keys of a tile
+constexpr int LEAST_TILES = 8;                    // of a part
 constexpr float LAZY = 8.f;                       // where maxima are taken, the reference may lag them this much (base 2)
 // A lane's 16 weights of a half may add up to this: in fp16 none of them is then beyond 65504; fp32 and bf16 end at 2^127.  Past
 // CALM the references are brought up with the next tile.
@@ -200,8 +201,9 @@ __global__ __launch_bounds__(64 * wavefronts(PAGED, DV), DV <= 128 ? 2 : 1) void
     const ServeDims &d = kp.d;
     const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, h32 = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // one KV head's items follow one another at a distance of S (an XCD sees few heads), the last rows first
-    const int u = kp.by_parts((int)blockIdx.x), part = blockIdx.x - u * kp.parts, y = d.by_S(u), x = kp.items - 1 - y, s = u - y * d.S;
+    // first part 0 of all items (every XCD has some of those that are not split); one KV head's items follow one another at a distance of S (an XCD sees
+    // few heads), the last rows first
+    const int part = kp.by_units((int)blockIdx.x), u = blockIdx.x - part * (kp.items * d.S), y = d.by_S(u), x = kp.items - 1 - y, s = u - y * d.S;
     int item0;
     const int b = request_of_item<BM>(kp.q_start, d, x, lane, item0);
     const Request r = make_request(kp.q_start, kp.seq_len, kp.prefix_len, b, d.T, d.max_blocks * d.page);
@@ -216,7 +218,7 @@ __global__ __launch_bounds__(64 * wavefronts(PAGED, DV), DV <= 128 ? 2 : 1) void
     const int w_lo = __builtin_amdgcn_readfirstlane(r.pos0 + d.by_hps(min(c_first + 32 * wave, columns - 1)));
     const int w_hi = __builtin_amdgcn_readfirstlane(r.pos0 + d.by_hps(min(c_first + 32 * wave + 31, columns - 1)));
     const Tiles tiles = make_tiles<BM>(d, kp.rule, r, c_first, columns);
-    const int per = max(kp.per_part, kp.by_parts(tiles.count + kp.parts - 1)), t_lo = part * per, n_tiles = min(tiles.count - t_lo, per);
+    const int per = max(LEAST_TILES, kp.by_parts(tiles.count + kp.parts - 1)), t_lo = part * per, n_tiles = min(tiles.count - t_lo, per);
     if (n_tiles <= 0 && part > 0) return;         // (nothing to see at all: part 0 writes it)
     const bool whole = n_tiles == tiles.count;
     // step t takes tile t_lo + t, counted backwards
@@ -649,7 +651,7 @@ __global__ __launch_bounds__(256) void scored_merge_kernel(const TileParams kp)
     const int columns = r.rows * d.hps, c_first = (x - item0) * BM;
     if (x < item0 || c_first >= columns || columns < kp.least) return;
     const Tiles tiles = make_tiles<BM>(d, kp.rule, r, c_first, columns);
-    const int per = max(kp.per_part, kp.by_parts(tiles.count + kp.parts - 1));
+    const int per = max(LEAST_TILES, kp.by_parts(tiles.count + kp.parts - 1));
     if (tiles.count <= per) return;               // one part: it has written the output
     const int parts = (tiles.count + per - 1) / per, c = c_first + k;
     const float *src = kp.part + ((size_t)u * kp.parts * BM + k) * (DV + 2);
@@ -704,7 +706,7 @@ constexpr int width_class(int dk, int dv) { return dk <= 64 && dv <= 64 ? 0 : dk
 constexpr int CLASS_DV[4] = {64, 128, 128, 256};
 
 // How a call is split, from its sizes and hints: items of BM columns, and where they alone do not fill the chip their tiles.
-struct Plan { int items, parts, per_part; };
+struct Plan { int items, parts; };
 Plan make_plan(const ServeDims &d, bool paged)
 {
     const int BM = 32 * wavefronts(paged, CLASS_DV[width_class(d.d_sel, d.d_pool)]);
@@ -714,10 +716,8 @@ Plan make_plan(const ServeDims &d, bool paged)
     const long tiles = std::max<long>(1, ((d.window > 0 ? std::min<long>(keys, (long)d.window + BM) : keys) + BN - 1) / BN);
     const long busy = std::max<long>(1, (long)d.T * d.hps / BM) * d.S;         // items that have work, about
     // As many workgroups as run at a time (eight wavefronts: one per CU, four: two), of eight tiles at least.  700 rows over 9000 tokens and five smaller
-    // requests, 32 heads over 8: 175 us for 256 workgroups, 169 for 560, 226 for 880 (rounds that end with few of them; where depends on lengths unknown here).
-    const long parts = std::max<long>(1, std::min<long>(1024 / (BM / 32) * 2 / busy, tiles / 8));
-    p.per_part = (int)((tiles + parts - 1) / parts);
-    p.parts = (int)((tiles + p.per_part - 1) / p.per_part);
+    // requests, 32 heads over 8: 167 us so (two parts), 215 with three, 193 with six: rounds that end with few of them.
+    p.parts = (int)std::max<long>(1, std::min<long>(1024 / (BM / 32) * 2 / busy, tiles / LEAST_TILES));
     return p;
 }
 
@@ -748,7 +748,7 @@ template <bool PAGED> hipError_t launch(const ScoredArgs &a, int least, hipStrea
 {
     const Plan p = make_plan(a.d, PAGED);
     const TileParams kp{a.Q, a.SEL, a.POOL, a.O, a.lse, a.q_start, a.seq_len, a.prefix_len, a.block_table, a.slopes, a.sel_q8, a.pool_q8, a.scales, a.d,
-                        score_rule(a.d), p.items, least, p.parts, p.per_part, FastDiv(p.parts), a.part};
+                        score_rule(a.d), p.items, least, p.parts, FastDiv(p.parts), FastDiv((int)((long)p.items * a.d.S)), a.part};
     if (a.d.dtype == LCA_F16) run_widths<_Float16, PAGED>(kp, st);
     else run_widths<__bf16, PAGED>(kp, st);
     return hipGetLastError();
