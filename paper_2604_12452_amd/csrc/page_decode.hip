@@ -14,7 +14,7 @@
 // A wavefront takes every W-th tile of 64 keys of its workgroup's part on its own (four of them, eight where a workgroup has a request and
 // a CU to itself); the loads of its next tile are issued as soon as the registers of this one are free.  Softmax with a running maximum, sums in fp32 of the
 // weights before they are rounded.  Parts of long requests are joined by page_merge_kernel.
-// 32 requests of 65536 tokens, 32 heads over 8, 128 / 128: 0.68 to 0.73 ms, 5.9 to 6.3 TB/s, what a plain read reaches (4.31 GB fetched, 4.30 needed).
+// 32 requests of 65536 tokens, 32 heads over 8, 128 / 128: 0.68 to 0.73 ms, 5.9 to 6.3 TB/s, what a plain read reaches (4.33 GB fetched, 4.30 needed).
 // One of 500 tokens, 28 heads over 4: 8.9 us, a chain of launch, starts, table, codes, join.
 #include <algorithm>
 
