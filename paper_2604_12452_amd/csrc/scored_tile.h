@@ -88,15 +88,16 @@ struct TileParams {
     const float *scales;
     ServeDims d;
     ScoreRule rule;
-    int items;                                    // per KV head
+    int items;                                    // numbers of work items, per KV head
+    bool by_slots;                                // how they are counted (request_of_item)
     int least;                                    // requests of fewer (row, head) pairs per KV head are another kernel's
     int parts;                                    // workgroups of an item
     FastDiv by_parts, by_units;                   // items * S
-    float *part;                                  // their results, [item, KV head, part, BM, DV + 2]
+    float *part;                                  // their results, [slot, KV head, part, BM, DV + 2]
 };
 
 // Wavefronts per workgroup (32 columns each): over the cache eight, so that a tile's codes are converted for 256 columns, unless
-// the width takes the registers of two wavefronts per SIMD.
+// the width takes the registers of two wavefronts per SIMD (the chunks above 187 us, 210 with four, before later steps).
 constexpr int wavefronts(bool paged, int dv) { return paged && dv <= 128 ? 8 : 4; }
 constexpr int BN = 64;                            // keys of a tile
 constexpr int LEAST_TILES = 8;                    // of a part
@@ -131,11 +132,18 @@ template <int N> __device__ __forceinline__ void copies(const unsigned *voff, co
     if constexpr (N > 4) copies<N - 4>(voff + 4, rs, at + 4096);
 }
 
-// The request of work item x (counted from the first): request b's items start at floor(q_start[b] * hps / BM) + b, which leaves
-// each at least as many numbers as it has items; 64 starts are looked at at a time.
-template <int BM> __device__ __forceinline__ int request_of_item(const int32_t *q_start, const ServeDims &d, int x, int lane, int &first)
+// The request of work item x (counted from the first); 64 starts are looked at at a time.  Request b's items start at floor(q_start[b] * hps / BM) + b, which
+// leaves each at least as many numbers as it has items; over the cache, where that is fewer numbers, at floor(q_start[b] * hps / 64): requests that are this
+// kernel's have 65 columns and more, room for their items, and those before and after them, however many, take no numbers of theirs (256 requests of one
+// token over 2000, max_q not known: 284 us, 357 by the first; 700 rows over 9000 tokens and five smaller requests 169.5, 166 by the first).
+constexpr int SLOT = 64;
+static_assert(PAGE_DECODE_COLUMNS >= SLOT, "floor(n / 64) >= ceil(n / 128) for n above 64");
+template <int BM> __device__ __forceinline__ int request_of_item(const int32_t *q_start, const ServeDims &d, bool by_slots, int x, int lane, int &first)
 {
-    auto start = [&](int b) __attribute__((always_inline)) { return (int)((long)min(max(q_start[b], 0), d.T) * d.hps / BM) + b; };
+    auto start = [&](int b) __attribute__((always_inline)) {
+        const long column = (long)min(max(q_start[b], 0), d.T) * d.hps;
+        return by_slots ? (int)(column / SLOT) : (int)(column / BM) + b;
+    };
     int lo = 0, n = d.B;                          // the request is one of [lo, lo + n): the last that starts at or before x
     while (n > 1) {
         const int step = (n + 63) / 64, b = min(lo + lane * step, lo + n - 1);
@@ -160,6 +168,9 @@ template <int BM> __device__ __forceinline__ Tiles make_tiles(const ServeDims &d
     t.count = t.pre + max((hi + BN) / BN - t.from, 0);
     return t;
 }
+
+// Where the parts of item k of a request lie (packed rows too: only documents of more than 64 LEAST_TILES rows are split).
+__device__ __forceinline__ size_t slot_of(const ServeDims &d, const Request &r, int k) { return (size_t)((long)r.first * d.hps / SLOT + k); }
 
 // A column that did not come out as finite numbers: again, over what its row sees alone (serve_row.h).
 template <typename E, int DV, bool PAGED>
@@ -205,10 +216,11 @@ __global__ __launch_bounds__(64 * wavefronts(PAGED, DV), DV <= 128 ? 2 : 1) void
     // few heads), the last rows first
     const int part = kp.by_units((int)blockIdx.x), u = blockIdx.x - part * (kp.items * d.S), y = d.by_S(u), x = kp.items - 1 - y, s = u - y * d.S;
     int item0;
-    const int b = request_of_item<BM>(kp.q_start, d, x, lane, item0);
+    const int b = request_of_item<BM>(kp.q_start, d, kp.by_slots, x, lane, item0);
     const Request r = make_request(kp.q_start, kp.seq_len, kp.prefix_len, b, d.T, d.max_blocks * d.page);
-    const int columns = r.rows * d.hps, c_first = (x - item0) * BM;
-    if (x < item0 || c_first >= columns || columns < kp.least) return;
+    const int columns = r.rows * d.hps, item = x - item0;
+    if (item < 0 || item >= (columns + BM - 1) / BM || columns < kp.least) return;
+    const int c_first = item * BM;
 
     // this lane's column
     const int c_lane = c_first + 32 * wave + n32, c = min(c_lane, columns - 1), row = d.by_hps(c), head = s * d.hps + (c - row * d.hps);
@@ -590,7 +602,7 @@ __global__ __launch_bounds__(64 * wavefronts(PAGED, DV), DV <= 128 ? 2 : 1) void
     // ---- output ----
     l_run = lanes::across32(l_run, lanes::Sum());
     if (!whole) {
-        float *dst = kp.part + (((size_t)u * kp.parts + part) * BM + 32 * wave + n32) * (DV + 2);
+        float *dst = kp.part + (((slot_of(d, r, item) * d.S + s) * kp.parts + part) * BM + 32 * wave + n32) * (DV + 2);
         if (h32 == 0) { dst[0] = m_run; dst[1] = l_run; }
 #pragma unroll
         for (int v = 0; v < NDV; ++v)
@@ -646,15 +658,16 @@ __global__ __launch_bounds__(256) void scored_merge_kernel(const TileParams kp)
     const int k = (blockIdx.x % (BM / 16)) * 16 + (threadIdx.x >> 4);
     const int y = d.by_S(u), x = kp.items - 1 - y, s = u - y * d.S;
     int item0;
-    const int b = request_of_item<BM>(kp.q_start, d, x, lane, item0);
+    const int b = request_of_item<BM>(kp.q_start, d, kp.by_slots, x, lane, item0);
     const Request r = make_request(kp.q_start, kp.seq_len, kp.prefix_len, b, d.T, d.max_blocks * d.page);
-    const int columns = r.rows * d.hps, c_first = (x - item0) * BM;
-    if (x < item0 || c_first >= columns || columns < kp.least) return;
+    const int columns = r.rows * d.hps, item = x - item0;
+    if (item < 0 || item >= (columns + BM - 1) / BM || columns < kp.least) return;
+    const int c_first = item * BM;
     const Tiles tiles = make_tiles<BM>(d, kp.rule, r, c_first, columns);
     const int per = max(LEAST_TILES, kp.by_parts(tiles.count + kp.parts - 1));
     if (tiles.count <= per) return;               // one part: it has written the output
     const int parts = (tiles.count + per - 1) / per, c = c_first + k;
-    const float *src = kp.part + ((size_t)u * kp.parts * BM + k) * (DV + 2);
+    const float *src = kp.part + ((slot_of(d, r, item) * d.S + s) * kp.parts * BM + k) * (DV + 2);
     constexpr size_t STEP = (size_t)BM * (DV + 2);
     float m = -INFINITY, l = 0.f, sum[N];
     for (int p = l16; p < parts; p += 16) m = fmaxf(m, src[p * STEP]);
@@ -706,12 +719,14 @@ constexpr int width_class(int dk, int dv) { return dk <= 64 && dv <= 64 ? 0 : dk
 constexpr int CLASS_DV[4] = {64, 128, 128, 256};
 
 // How a call is split, from its sizes and hints: items of BM columns, and where they alone do not fill the chip their tiles.
-struct Plan { int items, parts; };
+struct Plan { int items, parts; bool by_slots; };
 Plan make_plan(const ServeDims &d, bool paged)
 {
     const int BM = 32 * wavefronts(paged, CLASS_DV[width_class(d.d_sel, d.d_pool)]);
     Plan p;
-    p.items = (int)((long)d.T * d.hps / BM) + d.B;
+    const int apart = (int)((long)d.T * d.hps / BM) + d.B, slots = (int)((long)d.T * d.hps / SLOT) + 1;
+    p.by_slots = paged && slots < apart;
+    p.items = p.by_slots ? slots : apart;
     const long keys = paged ? d.max_kv : d.max_q;
     const long tiles = std::max<long>(1, ((d.window > 0 ? std::min<long>(keys, (long)d.window + BM) : keys) + BN - 1) / BN);
     const long busy = std::max<long>(1, (long)d.T * d.hps / BM) * d.S;         // items that have work, about
@@ -748,7 +763,7 @@ template <bool PAGED> hipError_t launch(const ScoredArgs &a, int least, hipStrea
 {
     const Plan p = make_plan(a.d, PAGED);
     const TileParams kp{a.Q, a.SEL, a.POOL, a.O, a.lse, a.q_start, a.seq_len, a.prefix_len, a.block_table, a.slopes, a.sel_q8, a.pool_q8, a.scales, a.d,
-                        score_rule(a.d), p.items, least, p.parts, FastDiv(p.parts), FastDiv((int)((long)p.items * a.d.S)), a.part};
+                        score_rule(a.d), p.items, p.by_slots, least, p.parts, FastDiv(p.parts), FastDiv((int)((long)p.items * a.d.S)), a.part};
     if (a.d.dtype == LCA_F16) run_widths<_Float16, PAGED>(kp, st);
     else run_widths<__bf16, PAGED>(kp, st);
     return hipGetLastError();

@@ -13,7 +13,7 @@ size_t scored_tile_workspace_bytes(const ServeDims &d, bool paged)
 {
     const Plan p = make_plan(d, paged);
     const int dv = CLASS_DV[width_class(d.d_sel, d.d_pool)];
-    return p.parts > 1 ? (size_t)p.items * d.S * p.parts * 32 * wavefronts(paged, dv) * (dv + 2) * sizeof(float) : 0;
+    return p.parts > 1 ? (size_t)((long)d.T * d.hps / SLOT + 1) * d.S * p.parts * 32 * wavefronts(paged, dv) * (dv + 2) * sizeof(float) : 0;
 }
 
 hipError_t launch_scored_tile(const ScoredArgs &a, hipStream_t st) { return launch<false>(a, 0, st); }

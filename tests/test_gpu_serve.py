@@ -454,6 +454,22 @@ def test_paged_long_and_any_hint(page, max_q, max_kv):
     _check_paged(rng, [70, 1], [900, 1500], 4, 1, 64, 64, page, "f16", RULES["all"], max_q=max_q, max_kv=max_kv, lse=False)
 
 
+@pytest.mark.parametrize("rows", [[1] * 20 + [90] + [0, 1, 2] * 10 + [33, 34] + [1] * 5, [33, 200, 1, 40] + [1] * 60, [0] * 50 + [300] + [0] * 50 + [65, 33, 65]])
+@pytest.mark.parametrize("max_kv", [0, 5000])
+def test_paged_chunks_among_many_small_requests(rows, max_kv):
+    """Work items are counted by rows where the requests are many; their parts lie by rows as well."""
+    rng = np.random.default_rng(len(rows))
+    lens = [n + int(rng.integers(1, 50)) + (1500 if n >= 90 else 0) for n in rows]
+    _check_paged(rng, rows, lens, 4, 2, 64, 64, 16, "bf16", RULES["window" if max_kv else "plain"] if rows[0] else dict(slopes=True), max_kv=max_kv)
+
+
+def test_packed_splits_among_many_small_documents():
+    rng = np.random.default_rng(17)
+    starts = np.cumsum([0] + [1, 0, 3] * 20 + [1200] + [2, 60] * 3 + [700] + [1] * 9).tolist()
+    x = [_randn(rng, "bf16", starts[-1] + 2, h, 64) for h in (3, 1, 1)]
+    _check_packed(*x, starts, "bf16", 0.125, RULES["plain"])
+
+
 def test_paged_rows_that_see_nothing():
     """More rows than tokens, requests of no tokens (refused ones), tables of numbers that are no blocks, lengths beyond the table."""
     rng = np.random.default_rng(21)

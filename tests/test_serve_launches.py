@@ -101,14 +101,30 @@ def test_what_no_matrix_kernel_takes_goes_row_by_row(kw):
     _desc(B=200, T=200, max_q=1), _desc(T=3000, B=2), _desc(T=70, B=1, max_kv=65536, d_pool=64, d_sel=64), _desc(T=500, B=1, H=2, S=2, max_blocks=0, n_blocks=0),
     _desc(T=9000, B=1, H=1, S=1, max_blocks=0, n_blocks=0), _desc(T=2000, B=30, H=4, S=4, d_pool=192, max_blocks=0, n_blocks=0)], ids=lambda d: f"B{d.B}-T{d.T}-H{d.H}-S{d.S}-{d.d_pool}")
 def test_the_partial_results_fit_the_workspace(d):
-    """A part's results are 16 NCT columns (decode) or as many as its workgroup has (32 per wavefront), the width and two numbers each."""
+    """A part's results are 16 NCT columns (decode) or as many as its workgroup has (32 per wavefront), the width and two numbers each; the tile kernels' lie in a slot
+    for every 64 (row, head) pairs, KV head and part, whatever the number of requests."""
     have = serve.workspace_size(d)
     for run in ([_paged(d)] if d.max_blocks else []) + [_packed(d)]:
         for i, r in enumerate(run):
             if "merge" not in r.kernel:
                 continue
             dv, columns = _name(run[i - 1])[2][1], 16 * _name(run[i - 1])[2][2] if "decode" in run[i - 1].kernel else run[i - 1].block // 2
-            assert run[i - 1].grid * columns * (dv + 2) * 4 <= have, (run[i - 1], have)
+            places = run[i - 1].grid
+            if "decode" not in run[i - 1].kernel:
+                pairs = d.T * d.H // d.S
+                slots, items = pairs // 64 + 1, pairs // columns + d.B
+                if _name(run[i - 1])[3][0] in (True, "true"):          # over the cache
+                    items = min(items, slots)
+                parts, rest = divmod(run[i - 1].grid, items * d.S)
+                assert rest == 0 and parts > 1
+                places = slots * d.S * parts
+            assert places * columns * (dv + 2) * 4 <= have, (run[i - 1], have)
+
+
+def test_the_workspace_does_not_grow_with_requests_of_one_token():
+    """The chunk kernel's part of it (no hints: it is launched) is a matter of the rows."""
+    small, large = (serve.workspace_size(_desc(T=256, B=b, max_kv=9000)) for b in (4, 256))
+    assert large <= 3 * small and large < 1 << 29
 
 
 def test_hints_never_make_a_grid_of_none():
