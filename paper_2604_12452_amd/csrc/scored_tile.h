@@ -126,9 +126,9 @@ constexpr int COPY_ROOM = 3 * 1024;
 template <int N> __device__ __forceinline__ void copies(const unsigned *voff, const int4v &rs, unsigned at)
 {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(voff[0]), "s"(rs), "s"(at) : "memory");
-    if constexpr (N > 1) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:1024 lds" : : "v"(voff[1]), "s"(rs) : "memory");
-    if constexpr (N > 2) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:2048 lds" : : "v"(voff[2]), "s"(rs) : "memory");
-    if constexpr (N > 3) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:3072 lds" : : "v"(voff[3]), "s"(rs) : "memory");
+    if constexpr (N > 1) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:%2 lds" : : "v"(voff[1]), "s"(rs), "n"(1 * 1024) : "memory");
+    if constexpr (N > 2) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:%2 lds" : : "v"(voff[2]), "s"(rs), "n"(2 * 1024) : "memory");
+    if constexpr (N > 3) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:%2 lds" : : "v"(voff[3]), "s"(rs), "n"(3 * 1024) : "memory");
     if constexpr (N > 4) copies<N - 4>(voff + 4, rs, at + 4096);
 }
 
