@@ -70,7 +70,7 @@ struct DecodeParams {
 };
 
 constexpr int TILE = 64;
-constexpr int LEAST_TILES = 8;            // of a part (24 requests of 4 rows, window 4096, in up to ten parts: 13.7 us, 14.3 with four, 16.9 with sixteen)
+constexpr int LEAST_TILES = 8;            // of a part (24 requests of 4 rows, window 4096, in up to ten parts: 13.7 us, 14.3 with four, 16.9 with sixteen; 14.1 since)
 // Whether a wavefront needs the registers of two.
 constexpr bool heavy(int dv, int nct) { return dv * nct >= 256; }
 
@@ -261,7 +261,10 @@ __global__ __launch_bounds__(64 * W, heavy(DV, NCT) ? 1 : 2) void page_decode_ke
                 float lg[16], mx = -INFINITY;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) lg[i] = sacc[ct][i >> 2][i & 3];
-                if (kp.rule.cap_log2 > 0.f) {
+                if (kp.rule.cap_log2 > 0.f && full) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) lg[i] = capped_among_many(lg[i], kp.rule);
+                } else if (kp.rule.cap_log2 > 0.f) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) lg[i] = capped<true>(lg[i], kp.rule);
                 } else {

@@ -109,11 +109,18 @@ inline ScoreRule score_rule(float scale, float softcap, int window)
 }
 inline ScoreRule score_rule(const ServeDims &d) { return score_rule(d.scale, d.softcap, d.window); }
 inline bool in_fp32(const ScoreRule &r) { return std::isfinite(r.scale_log2) && std::isfinite(2.f * r.cap_log2) && std::isfinite(r.pre); }
+// Below a quarter of the cap the difference would lose what the score has: tanh's series there (next term 2^-26 of the score), a few 2^-24 of the score
+// itself.  Tiles of 64 keys that every row sees whole do without: their sums hide it (24 requests, window 4096: 14.1 us, 14.7 with the series in all).
+__device__ __forceinline__ float capped_among_many(float dot, const ScoreRule &r)
+{
+    return fmaf(-2.f * r.cap_log2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(dot * r.pre)), r.cap_log2);
+}
 template <bool CAP> __device__ __forceinline__ float capped(float dot, const ScoreRule &r)
 {
     if constexpr (!CAP) return dot * r.scale_log2;
-    const float e = __builtin_amdgcn_exp2f(dot * r.pre);
-    return fmaf(-2.f * r.cap_log2, __builtin_amdgcn_rcpf(1.f + e), r.cap_log2);
+    const float u = dot * r.pre * (0.5f / LOG2E), v = u * u;
+    const float series = fmaf(v, fmaf(v, fmaf(v, fmaf(v, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+    return v < 0.0625f ? dot * r.scale_log2 * series : capped_among_many(dot, r);
 }
 
 // The request whose rows hold row t: the last one that starts at or in front of t (empty ones share their start with the

@@ -318,6 +318,26 @@ def test_packed_large_logits(dtype):
     _check_packed(Q, SEL, POOL, [0, T], dtype, 2.0, dict(softcap=200.0, window=100))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_caps_far_above_the_scores_of_few_keys(dtype):
+    """lse of rows that see up to three keys, scores of a hundredth of the cap: the bound is that of no cap (its slope is at most one), and 2^-20 of the logits for the
+    series, its argument and the change of base, not 2^-22 of the cap."""
+    rng = np.random.default_rng(9)
+    torch, lca, serve = _api()
+    T, cap = 48, 500.0
+    Q, SEL, POOL = (_randn(rng, dtype, T, 2, 64) for _ in range(3))
+    d = serve.Desc(B=16, T=T, H=2, S=2, d_pool=64, d_sel=64, dtype=_code(dtype), scale=0.125, softcap=cap)
+    O, lse = torch.empty_like(Q), torch.empty(T, 2, device="cuda")
+    serve.packed_attn(d, Q, SEL, POOL, _i32(range(0, T + 1, 3)), None, None, O, lse, serve.alloc_workspace(d))
+    for h in range(2):
+        q, k, v = _f64(Q)[:, h], _f64(SEL)[:, h], _f64(POOL)[:, h]
+        for lo in range(0, T, 3):
+            r = slice(lo, lo + 3)
+            want = ref.attend(q[r], k[r], v[r], np.arange(3), 3, dtype, scale=0.125, softcap=cap)
+            bound = ref.attend(q[r], k[r], v[r], np.arange(3), 3, dtype, scale=0.125)
+            _close(_f64(lse)[r, h], want[1], bound[3] + 2.0 ** -20 * 0.125 * np.abs(q[r] @ k[r].T).max(), (lo, h, "lse"))
+
+
 @pytest.mark.parametrize("softcap", [1024.0, 1e6])
 def test_packed_fp32_caps_far_above_the_scores(softcap):
     """The cap bends scores of a few units by next to nothing and must not cost them its own 2^-24: the bound is that of no cap (its slope is at most one),
